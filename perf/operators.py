@@ -1,0 +1,543 @@
+"""The streaming operators as measurable cases: windowed attention and the 8-bit cache.
+
+A model that generates a long video (or text) piece by piece is trained with attention whose keys are a window of the
+past and the first few frames (or tokens), and generates with a cache of the keys and values it has seen:
+
+  fwd      windowed attention, forward (`WindowBuffers.forward`): sampling a whole clip, reading a prompt
+  train    the same, forward and backward (`WindowBuffers.backward`)
+  append   new keys and values into the pages of the 8-bit cache (`PagedCache.append`)
+  attend   attention of one token, or of a chunk of them, over that cache (`PagedCache.attend`)
+
+A position x lies in unit x // unit (unit = 1: tokens; the tokens of a frame: frames).  The last query stands at the last
+key.  Key j is visible to a query at position p if j's unit is at most p's unit + right, and at least p's unit - left or
+among the first `sinks` units; a negative left or right is no bound.
+
+A cache page holds 64 tokens: keys [Hkv, 64, d], values [Hkv, d, 64], in e4m3, and a scale a head for each, a power of two:
+the smallest that brings the page's largest value to 448 or less.  Inputs are synthetic and seeded.
+"""
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+PAGE = 64
+TOP = 448.0       # the largest e4m3 value
+LOWEST = -60      # exponent of the smallest scale
+DTYPES = {"bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def _window(name, op, lens_q, lens_k, H, Hkv, d, left, right, sinks, unit, dtype="bf16", packed=False, fused=False):
+    return dict(name=name, op=op, lens_q=",".join(map(str, lens_q)), lens_k=",".join(map(str, lens_k)), H=H, Hkv=Hkv, d=d, left=left,
+                right=right, sinks=sinks, unit=unit, dtype=dtype, packed=packed, fused=fused)
+
+
+def _cache(name, op, lens, new, H, Hkv, d, left=-1, right=0, sinks=0, unit=1, dtype="bf16"):
+    """lens: tokens of each sequence with the new ones; new: how many of them are new (append) or ask (attend)."""
+    return dict(name=name, op=op, lens=",".join(map(str, lens)), new=",".join(map(str, new)), H=H, Hkv=Hkv, d=d, left=left, right=right,
+                sinks=sinks, unit=unit, dtype=dtype)
+
+
+def _ragged(seed, n, low, high):
+    """n lengths, spread over the logarithm."""
+    rng = random.Random(seed)
+    return [int(round(math.exp(rng.uniform(math.log(low), math.log(high))))) for _ in range(n)]
+
+
+def listed():
+    packed = [1, 4099, 700, 17, 6001, 64, 2503]
+    train_packed = [3001, 5, 1, 2048, 777, 4500]
+    return [
+        # a small clip, 8 frames of 256 tokens, causal over frames: launches are most of it
+        _window("clip_fwd", "fwd", [2048], [2048], 2, 2, 64, 2, 0, 1, 256),
+        # prompts of a language-model-like mixture, one token to 6001, four query heads a key head, packed one behind the other
+        _window("prompts_fwd", "fwd", packed, packed, 16, 4, 128, 1023, 0, 4, 1, dtype="f16", packed=True),
+        # 480p clip, 21 frames of 1560 tokens: a window of seven frames and the first one; q, k, v as the projection leaves them
+        _window("frames480_fwd", "fwd", [32760], [32760], 12, 12, 128, 6, 0, 1, 1560, fused=True),
+        # training: the small clip
+        _window("clip_train", "train", [2048], [2048], 2, 2, 64, 2, 0, 1, 256),
+        # training on packed texts with shared key heads, token windows
+        _window("packed_train", "train", train_packed, train_packed, 16, 4, 64, 511, 0, 4, 1, packed=True),
+        # training: the pretraining-sized latent, 16 frames of 1024 tokens
+        _window("frames_train", "train", [16384], [16384], 12, 12, 128, 3, 0, 1, 1024, fused=True),
+        # one token for each of 16 sequences, anywhere in its page
+        _cache("append_token", "append", _ragged(1, 16, 65, 4096), [1] * 16, 4, 4, 128),
+        # a 480p frame for each of two streams, behind what is there
+        _cache("append_frame", "append", [1560 * 3 + 7, 1560 * 2], [1560, 1560], 12, 12, 128),
+        # a whole 720p clip
+        _cache("append_clip", "append", [75600], [75600], 40, 40, 128),
+        # one token each for a few short sequences: latency
+        _cache("token_short", "attend", [37, 900, 1500, 2011], [1] * 4, 16, 4, 128),
+        # one token each for sequences up to long ones: the cache is read once
+        _cache("token_long", "attend", _ragged(2, 16, 1000, 131072), [1] * 16, 16, 4, 128, dtype="f16"),
+        # a 480p frame against the window of frames that the cache holds
+        _cache("frame_chunk", "attend", [1560 * 21], [1560], 12, 12, 128, 6, 0, 1, 1560),
+    ]
+
+
+def _ints(text):
+    return [int(x) for x in text.split(",")]
+
+
+def _rows(case):
+    """Per sequence: (queries, keys)."""
+    if "lens_q" in case:
+        return list(zip(_ints(case["lens_q"]), _ints(case["lens_k"])))
+    return list(zip(_ints(case["new"]), _ints(case["lens"])))
+
+
+def _span(pos, case, keys):
+    """Of the queries at positions `pos` (a numpy array): first key of the window, end of the window, end of the sinks."""
+    u = np.floor_divide(pos, case["unit"])
+    end = np.full_like(pos, keys) if case["right"] < 0 else np.clip((u + case["right"] + 1) * case["unit"], 0, keys)
+    first = np.zeros_like(pos) if case["left"] < 0 else np.clip((u - case["left"]) * case["unit"], 0, None)
+    return np.minimum(first, end), end, np.minimum(min(case["sinks"] * case["unit"], keys), end)
+
+
+def _pairs(case):
+    """Visible pairs of all sequences, and keys that any query of them sees."""
+    pairs = seen = 0
+    for nq, nk in _rows(case):
+        if nq == 0 or nk == 0:
+            continue
+        first, end, sink = _span(np.arange(nq, dtype=np.int64) + (nk - nq), case, nk)
+        pairs += int((end - first + np.minimum(sink, first)).sum())
+        seen += int(end[-1] - first[0] + min(sink[-1], first[0]))
+    return pairs, seen
+
+
+def _cost(case):
+    if case["op"] == "append":
+        return sum(_ints(case["new"])) * case["Hkv"] * case["d"] * 6e-3
+    w = work(case)
+    return w["flops"] * 1e-6 + w["bytes"] * 2e-4
+
+
+def work(case):
+    H, Hkv, d = case["H"], case["Hkv"], case["d"]
+    if case["op"] == "append":
+        new = sum(_ints(case["new"]))
+        pages = sum((n + PAGE - 1) // PAGE - (n - m) // PAGE for m, n in _rows(case))
+        return {"bytes": new * Hkv * d * 2 * (2 + 1) + pages * Hkv * 2 * 4, "flops": 2 * new * Hkv * d}
+    pairs, seen = _pairs(case)
+    nq, nk = (sum(x) for x in zip(*_rows(case)))
+    q, kv = nq * H * d * 2, nk * Hkv * d * 2
+    if case["op"] == "attend":
+        return {"bytes": 2 * q + seen * Hkv * d * 2 + (seen // PAGE) * Hkv * 8, "flops": 4 * d * H * pairs}
+    if case["op"] == "fwd":
+        return {"bytes": 2 * q + 2 * kv, "flops": 4 * d * H * pairs}
+    # forward and backward: q, k, v, dout in, out and three gradients out
+    return {"bytes": 4 * q + 4 * kv, "flops": 14 * d * H * pairs}
+
+
+def draw(rng):
+    limit = {c["op"]: 0.0 for c in listed()}
+    for c in listed():
+        limit[c["op"]] = max(limit[c["op"]], _cost(c))
+
+    def log(low, high):
+        return int(round(math.exp(rng.uniform(math.log(low), math.log(high)))))
+
+    while True:
+        op = rng.choice(["fwd", "train", "append", "attend", "attend"])
+        d = rng.choice([64, 128, 128])
+        Hkv = rng.choice([1, 2, 3, 4, 8, 12])
+        H = Hkv * rng.choice([1, 1, 2, 4, 5, 8])
+        dtype = rng.choice(["bf16", "bf16", "f16"])
+        frames = rng.random() < 0.5
+        unit = log(60, 1600) if frames else 1
+        left = rng.choice([-1, rng.randint(0, 8)]) if frames else rng.choice([-1, log(1, 4096)])
+        sinks = rng.choice([0, 1, 2]) if frames else rng.choice([0, 4, rng.randint(1, 130)])
+        if op in ("fwd", "train"):
+            right = rng.choice([0, 0, 0, -1, rng.randint(0, 2) * (1 if frames else 50)])
+            n = rng.choice([1, 2, rng.randint(3, 9)])
+            packed = n > 2 or rng.random() < 0.3
+            lens_k = [log(1, 20000 // n) for _ in range(n)] if packed else [log(100, 34000 // n)] * n
+            shorter = rng.random() < 0.2  # fewer queries than keys: a later piece of the sequences
+            lens_q = [max(1, x - rng.randint(0, x - 1)) for x in lens_k] if shorter else lens_k
+            if not packed:
+                lens_q = [lens_q[0]] * n
+            case = _window("", op, lens_q, lens_k, H, Hkv, d, left, right, sinks, unit, dtype, packed, fused=not packed and rng.random() < 0.5 and lens_q == lens_k)
+        elif op == "append":
+            n = rng.choice([1, 2, rng.randint(3, 32)])
+            new = [rng.choice([1, log(1, 60000 // n)]) for _ in range(n)]
+            case = _cache("", op, [x + rng.choice([0, log(1, 3000)]) for x in new], new, H, Hkv, d, dtype=dtype)
+        else:
+            n = rng.choice([1, 2, rng.randint(3, 32)])
+            lens = [log(1, 200000 // n) for _ in range(n)]
+            new = [1] * n if rng.random() < 0.6 else [min(x, log(1, 2000)) for x in lens]
+            case = _cache("", op, lens, new, H, Hkv, d, left, 0, sinks, unit, dtype)
+        if _cost(case) > limit[op]:
+            continue
+        del case["name"]
+        return case
+
+
+def _generator(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(seed) + 20250513)
+    return g
+
+
+def _randn(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda")
+
+
+def _offsets(lens):
+    return torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32, device="cuda")
+
+
+def _keys(g, n, heads, d):
+    """Keys have a few channels that are larger than the others, and an offset that all tokens share."""
+    gain = 0.7 + 1.3 * torch.rand(heads, d, generator=g, device="cuda") ** 4
+    return _randn(g, n, heads, d) * gain + 0.3 * _randn(g, heads, d)
+
+
+def _scale_of(amax):
+    """The smallest power of two that brings `amax` to TOP or less (integers of the exponent: no rounding)."""
+    m, e = torch.frexp(amax.float())
+    e = e - 9 + (m > TOP / 512).to(e.dtype)  # TOP = 0.875 * 2^9
+    e = torch.where(amax > 0, e, torch.full_like(e, LOWEST)).clamp(min=LOWEST)
+    return torch.ldexp(torch.ones_like(amax, dtype=torch.float32), e)
+
+
+def _quantised(x, scale):
+    return (x.float() / scale).to(torch.float8_e4m3fn)
+
+
+def _pages(g, case, lens):
+    """A page table for sequences of these lengths in a pool that is a little larger, in no order."""
+    need = [(n + PAGE - 1) // PAGE for n in lens]
+    order = torch.randperm(sum(need) + 3, generator=g, device="cuda").to(torch.int32)
+    table = torch.full((len(lens), max(max(need), 1)), -1, dtype=torch.int32, device="cuda")
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+    return table, sum(need) + 3
+
+
+def _fill(g, pages, heads, d):
+    """A pool of pages as earlier calls left it."""
+    k8 = torch.empty(pages, heads, PAGE, d, dtype=torch.float8_e4m3fn, device="cuda")
+    v8 = torch.empty(pages, heads, d, PAGE, dtype=torch.float8_e4m3fn, device="cuda")
+    ks = torch.empty(pages, heads, device="cuda")
+    vs = torch.empty(pages, heads, device="cuda")
+    gain = 0.7 + 1.3 * torch.rand(heads, 1, d, generator=g, device="cuda") ** 4
+    step = max(1, (1 << 26) // (heads * PAGE * d))
+    for a in range(0, pages, step):
+        b = min(pages, a + step)
+        k = _randn(g, b - a, heads, PAGE, d) * gain
+        v = _randn(g, b - a, heads, d, PAGE)
+        ks[a:b], vs[a:b] = _scale_of(k.abs().amax((2, 3))), _scale_of(v.abs().amax((2, 3)))
+        k8[a:b], v8[a:b] = _quantised(k, ks[a:b, :, None, None]), _quantised(v, vs[a:b, :, None, None])
+    return k8, v8, ks, vs
+
+
+def prepare(case, seed):
+    g = _generator(seed)
+    t, H, Hkv, d = DTYPES[case["dtype"]], case["H"], case["Hkv"], case["d"]
+    s = {"case": case}
+    rows = _rows(case)
+    nq, nk = (sum(x) for x in zip(*rows))
+    if case["op"] in ("fwd", "train"):
+        B = len(rows)
+        q, k, v = 1.3 * _randn(g, nq, H, d), _keys(g, nk, Hkv, d), _randn(g, nk, Hkv, d)
+        dout = _randn(g, nq, H, d).to(t) if case["op"] == "train" else None
+        if case["fused"]:
+            qkv = torch.cat([q, k, v], 1).to(t)
+            q, k, v = qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:]
+        else:
+            q, k, v = q.to(t), k.to(t), v.to(t)
+        s["cu_q"] = s["cu_k"] = None
+        if case["packed"]:
+            s["cu_q"], s["cu_k"] = _offsets([x for x, _ in rows]), _offsets([x for _, x in rows])
+        else:
+            q, k, v = (x.unflatten(0, (B, -1)) for x in (q, k, v))
+            dout = None if dout is None else dout.unflatten(0, (B, -1))
+        s.update(q=q, k=k, v=v, dout=dout)
+        if own:
+            from paper_2505_13389_amd import window
+            pb = window.WindowProblem(B=B, H=H, Hkv=Hkv, d=d, max_q=max(x for x, _ in rows), max_k=max(x for _, x in rows),
+                                      left=case["left"], right=case["right"], sinks=case["sinks"], unit=case["unit"], dtype=t,
+                                      total_q=nq if case["packed"] else 0, total_k=nk if case["packed"] else 0)
+            s["buf"] = window.WindowBuffers(pb, backward=case["op"] == "train")
+        return s
+    lens, new = _ints(case["lens"]), _ints(case["new"])
+    table, pages = _pages(g, case, lens)
+    k8, v8, ks, vs = _fill(g, pages, Hkv, d)
+    s.update(table=table, cu=_offsets(new), k8=k8, v8=v8, ks=ks, vs=vs)
+    s["lens"] = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    s["before"] = s["lens"] - torch.tensor(new, dtype=torch.int32, device="cuda")
+    if case["op"] == "append":
+        s["k"], s["v"] = _keys(g, nq, Hkv, d).to(t), _randn(g, nq, Hkv, d).to(t)
+    else:
+        s["q"] = (1.3 * _randn(g, nq, H, d)).to(t)
+    if own:
+        from paper_2505_13389_amd import window
+        s["cache"] = window.PagedCache.of(k8, v8, ks, vs)
+    return s
+
+
+# ---- plain forms
+
+def _visible(case, nq, nk, r0, r1, k0, k1):
+    """Which of the keys k0.. of a sequence the queries r0.. see."""
+    p = torch.arange(r0, r1, device="cuda")[:, None] + (nk - nq)
+    j = torch.arange(k0, k1, device="cuda")[None, :]
+    up, uj = torch.div(p, case["unit"], rounding_mode="floor"), torch.div(j, case["unit"], rounding_mode="floor")
+    see = torch.ones(r1 - r0, k1 - k0, dtype=torch.bool, device="cuda")
+    if case["right"] >= 0:
+        see &= uj <= up + case["right"]
+    if case["left"] >= 0:
+        see &= (uj >= up - case["left"]) | (uj < case["sinks"])
+    return see
+
+
+def _blocks(case, nq, nk, H):
+    """Rows of a sequence in pieces whose scores fit, and the keys that a piece can see."""
+    r = 0
+    while r < nq:
+        rows = min(nq - r, 2048)
+        while True:
+            first, end, sink = _span(np.array([r + nk - nq, r + rows - 1 + nk - nq]), case, nk)
+            if rows == 1 or H * rows * (int(end[1]) + 1) <= 1 << 28:
+                break
+            rows = (rows + 1) // 2
+        k0 = 0 if int(sink[1]) > 0 else int(first[0])
+        yield r, r + rows, k0, max(int(end[1]), k0)
+        r += rows
+
+
+def _attend_plain(case, q, k, v, dout=None):
+    """One sequence, 32 bits: q [H,nq,d], k, v [Hkv,nk,d].  With `dout` the gradients too."""
+    H, nq, d = q.shape
+    Hkv, nk, _ = k.shape
+    scale = 1 / math.sqrt(d)
+    out = torch.zeros_like(q)
+    dq, dk, dv = (torch.zeros_like(x) for x in (q, k, v)) if dout is not None else (None,) * 3
+    for r0, r1, k0, k1 in _blocks(case, nq, nk, H):
+        if k1 == k0:
+            continue
+        see = _visible(case, nq, nk, r0, r1, k0, k1)
+        qb = q[:, r0:r1].reshape(Hkv, -1, d)
+        kb, vb = k[:, k0:k1], v[:, k0:k1]
+        s = torch.matmul(qb, kb.transpose(1, 2)).view(H, r1 - r0, k1 - k0) * scale
+        s.masked_fill_(~see, -math.inf)
+        m = s.amax(-1, keepdim=True)
+        p = torch.exp(s - torch.where(torch.isinf(m), torch.zeros_like(m), m))
+        n = p.sum(-1, keepdim=True)
+        p = p / torch.where(n > 0, n, torch.ones_like(n))
+        pg = p.view(Hkv, -1, k1 - k0)
+        o = torch.matmul(pg, vb).view(H, r1 - r0, d)
+        out[:, r0:r1] = o
+        if dout is None:
+            continue
+        db = dout[:, r0:r1]
+        dg = db.reshape(Hkv, -1, d)
+        dv[:, k0:k1] += torch.matmul(pg.transpose(1, 2), dg)
+        ds = torch.matmul(dg, vb.transpose(1, 2)).view_as(p)
+        ds = p * (ds - (db * o).sum(-1, keepdim=True)) * scale
+        dsg = ds.view(Hkv, -1, k1 - k0)
+        dq[:, r0:r1] = torch.matmul(dsg, kb).view(H, r1 - r0, d)
+        dk[:, k0:k1] += torch.matmul(dsg.transpose(1, 2), qb)
+    return out, dq, dk, dv
+
+
+def _window_plain(s):
+    case = s["case"]
+    rows, shape, t = _rows(case), s["q"].shape, s["q"].dtype
+    q, k, v = (s[n].reshape(-1, *s[n].shape[-2:]) for n in ("q", "k", "v"))
+    dout = None if s["dout"] is None else s["dout"].reshape(q.shape)
+    parts, a, b = [], 0, 0
+    for nq, nk in rows:
+        x = [q[a:a + nq], k[b:b + nk], v[b:b + nk]] + ([] if dout is None else [dout[a:a + nq]])
+        got = _attend_plain(case, *(y.float().transpose(0, 1) for y in x))
+        parts.append([None if y is None else y.transpose(0, 1).to(t) for y in got])
+        a, b = a + nq, b + nk
+    whole = [torch.cat(x) for x in zip(*parts) if x[0] is not None]
+    out = {"out": whole[0].reshape(shape)}
+    if dout is not None:
+        out.update(dq=whole[1].reshape(shape), dk=whole[2].reshape(s["k"].shape), dv=whole[3].reshape(s["k"].shape))
+    return out
+
+
+def _append_plain(s):
+    k8, v8, ks, vs, heads = s["k8"], s["v8"], s["ks"], s["vs"], s["case"]["Hkv"]
+    at = 0
+    for b, (m, n) in enumerate(_rows(s["case"])):
+        if m == 0:
+            continue
+        start = n - m
+        p0, p1 = start // PAGE, (n + PAGE - 1) // PAGE
+        ids = s["table"][b, p0:p1].long()
+        pad = (p1 - p0) * PAGE
+        held, lo = start - p0 * PAGE, start - p0 * PAGE
+        for new, pool, scales, turn in ((s["k"], k8, ks, False), (s["v"], v8, vs, True)):
+            x = torch.zeros(pad, *new.shape[1:], device="cuda")
+            x[lo:lo + m] = new[at:at + m].float()
+            x = x.view(p1 - p0, PAGE, heads, -1).transpose(1, 2)  # [pages, heads, tokens, d]
+            scale = _scale_of(x.abs().amax((2, 3)))
+            old, old_scale = pool[ids].float(), scales[ids]
+            if held:  # the first page holds tokens: their scale stays unless the new ones need a larger one
+                scale[0] = torch.maximum(scale[0], old_scale[0])
+            x8 = _quantised(x, scale[:, :, None, None])
+            if turn:
+                x8 = x8.transpose(2, 3)
+            old8 = _quantised(old * old_scale[:, :, None, None], scale[:, :, None, None])
+            slot = torch.arange(pad, device="cuda").view(p1 - p0, 1, PAGE)
+            slot = slot[:, :, None, :] if turn else slot[:, :, :, None]
+            was = pool[ids].view(torch.uint8)
+            kept = torch.where(slot < lo, old8.view(torch.uint8), was)
+            pool.view(torch.uint8)[ids] = torch.where((slot >= lo) & (slot < lo + m), x8.contiguous().view(torch.uint8), kept)
+            scales[ids] = scale
+        at += m
+    return {"k": k8, "v": v8, "k_scale": ks, "v_scale": vs}
+
+
+def _cached(s, b, n):
+    """Keys and values [Hkv, n, d] of a sequence, as the cache holds them."""
+    ids = s["table"][b, :(n + PAGE - 1) // PAGE].long()
+    k = s["k8"][ids].float() * s["ks"][ids][:, :, None, None]
+    v = s["v8"][ids].float() * s["vs"][ids][:, :, None, None]
+    return k.transpose(0, 1).flatten(1, 2)[:, :n], v.permute(1, 0, 3, 2).flatten(1, 2)[:, :n]
+
+
+def _attend_cache_plain(s):
+    case, out, at = s["case"], torch.zeros_like(s["q"]), 0
+    for b, (nq, n) in enumerate(_rows(case)):
+        k, v = _cached(s, b, n)
+        o = _attend_plain(case, s["q"][at:at + nq].float().transpose(0, 1), k, v)[0]
+        out[at:at + nq] = o.transpose(0, 1).to(out.dtype)
+        at += nq
+    return {"out": out}
+
+
+def run(state):
+    s, case = state, state["case"]
+    op = case["op"]
+    if not own:
+        return _append_plain(s) if op == "append" else _attend_cache_plain(s) if op == "attend" else _window_plain(s)
+    if op == "append":
+        c = s["cache"]
+        c.append(s["k"], s["v"], s["table"], s["before"], cu=s["cu"], max_new=max(_ints(case["new"])))
+        return {"k": c.k, "v": c.v, "k_scale": c.k_scale, "v_scale": c.v_scale}
+    if op == "attend":
+        out = s["cache"].attend(s["q"], s["table"], s["lens"], cu=s["cu"], max_q=max(_ints(case["new"])), left=case["left"], right=case["right"],
+                                sinks=case["sinks"], unit=case["unit"])
+        return {"out": out}
+    buf = s["buf"]
+    buf.forward(s["q"], s["k"], s["v"], cu_q=s["cu_q"], cu_k=s["cu_k"])
+    if op == "fwd":
+        return {"out": buf.out}
+    buf.backward(s["q"], s["k"], s["v"], s["dout"], cu_q=s["cu_q"], cu_k=s["cu_k"])
+    return {"out": buf.out, "dq": buf.dq, "dk": buf.dk, "dv": buf.dv}
+
+
+# ---- from the definition, in 64 bits
+
+def _exact_head(case, q, k, v, dout):
+    """One sequence and query head: q [nq,d], k, v [nk,d].  Rows in pieces, all keys."""
+    nq, nk, d = q.shape[0], k.shape[0], q.shape[1]
+    out = torch.zeros_like(q)
+    dq, dk, dv = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    j = torch.arange(nk, device="cuda") // case["unit"]
+    step = max(1, min(nq, (1 << 27) // max(nk, 1)))
+    for a in range(0, nq, step):
+        p = torch.arange(a, min(nq, a + step), device="cuda") + nk - nq
+        u = (p - p.remainder(case["unit"])) // case["unit"]
+        hidden = torch.zeros(len(p), nk, dtype=torch.bool, device="cuda")
+        if case["left"] >= 0:
+            hidden = (j[None] < (u - case["left"])[:, None]) & (j[None] >= case["sinks"])
+        if case["right"] >= 0:
+            hidden = hidden | (j[None] > (u + case["right"])[:, None])
+        logits = (q[a:a + len(p)] @ k.t()) / d ** 0.5
+        logits[hidden] = -math.inf
+        total = torch.logsumexp(logits, 1, keepdim=True)
+        w = torch.exp(logits - torch.nan_to_num(total, neginf=0.0))
+        o = w @ v
+        out[a:a + len(p)] = o
+        if dout is not None:
+            do = dout[a:a + len(p)]
+            dv += w.t() @ do
+            dl = w * (do @ v.t() - (w * (do @ v.t())).sum(1, keepdim=True))
+            dq[a:a + len(p)] = dl @ k / d ** 0.5
+            dk += dl.t() @ q[a:a + len(p)] / d ** 0.5
+    return out, dq, dk, dv
+
+
+def _exact_e4m3(x):
+    """The nearest e4m3 value, ties to even, of |x| <= 448."""
+    _, e = torch.frexp(x)
+    step = torch.ldexp(torch.ones_like(x), (e - 1).clamp(min=-6) - 3)
+    return torch.round(x / step) * step
+
+
+def _exact_append(s):
+    """Token by token as the definition has it: of each page touched, the scale of what it holds then."""
+    case, heads = s["case"], s["case"]["Hkv"]
+    out = {"k": s["k8"].double(), "v": s["v8"].double(), "k_scale": s["ks"].double(), "v_scale": s["vs"].double()}
+    table, at = s["table"].cpu().numpy(), 0
+    for b, (m, n) in enumerate(_rows(case)):
+        start, done = n - m, 0
+        while done < m:
+            pos = start + done
+            page, slot = int(table[b, pos // PAGE]), pos % PAGE
+            count = min(PAGE - slot, m - done)
+            for name in ("k", "v"):
+                new = s[name][at + done:at + done + count].double().transpose(0, 1)  # [heads, tokens, d]
+                top = new.abs().amax((1, 2))
+                e = torch.ceil(torch.log2(top / TOP)).nan_to_num(neginf=LOWEST).clamp(min=LOWEST)
+                scale = torch.pow(torch.full_like(e, 2.0), e)
+                pool = out[name][page] if name == "k" else out[name][page].transpose(1, 2)  # [heads, tokens, d]
+                if slot:
+                    was = out[name + "_scale"][page].clone()
+                    scale = torch.maximum(scale, was)
+                    pool[:, :slot] = _exact_e4m3(pool[:, :slot] * (was / scale)[:, None, None])
+                pool[:, slot:slot + count] = _exact_e4m3(new / scale[:, None, None])
+                out[name + "_scale"][page] = scale
+            done += count
+        at += m
+    return out
+
+
+def exact(case, seed):
+    if case["op"] == "append":
+        if sum((m + PAGE) // PAGE + 1 for m, _ in _rows(case)) > 3000 or sum(_ints(case["lens"])) * case["Hkv"] * case["d"] > 1 << 28:
+            return None
+        return _exact_append(prepare(case, seed))
+    if sum(a * b for a, b in _rows(case)) * case["H"] * (3 if case["op"] == "train" else 1) > 2e10:
+        return None
+    s = prepare(case, seed)
+    H, group, rows = case["H"], case["H"] // case["Hkv"], _rows(case)
+    q = s["q"].double().reshape(-1, H, case["d"])
+    out = torch.zeros_like(q)
+    if case["op"] == "attend":
+        at = 0
+        for b, (nq, n) in enumerate(rows):
+            ids = s["table"][b, :-(-n // PAGE)].long()
+            for h in range(case["Hkv"]):
+                k = (s["k8"][ids, h].double() * s["ks"][ids, h].double()[:, None, None]).flatten(0, 1)[:n]
+                v = (s["v8"][ids, h].double() * s["vs"][ids, h].double()[:, None, None]).transpose(1, 2).flatten(0, 1)[:n]
+                for i in range(h * group, (h + 1) * group):
+                    out[at:at + nq, i] = _exact_head(case, q[at:at + nq, i], k, v, None)[0]
+            at += nq
+        return {"out": out}
+    k, v = (s[x].double().reshape(-1, case["Hkv"], case["d"]) for x in ("k", "v"))
+    dout = None if case["op"] == "fwd" else s["dout"].double().reshape(q.shape)
+    dq, dk, dv = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    a = b = 0
+    for nq, nk in rows:
+        for h in range(H):
+            g = h // group
+            got = _exact_head(case, q[a:a + nq, h], k[b:b + nk, g], v[b:b + nk, g], None if dout is None else dout[a:a + nq, h])
+            out[a:a + nq, h], dq[a:a + nq, h] = got[0], got[1]
+            dk[b:b + nk, g] += got[2]
+            dv[b:b + nk, g] += got[3]
+        a, b = a + nq, b + nk
+    answer = {"out": out.reshape(s["q"].shape)}
+    if dout is not None:
+        answer.update(dq=dq.reshape(s["q"].shape), dk=dk.reshape(s["k"].shape), dv=dv.reshape(s["k"].shape))
+    return answer
