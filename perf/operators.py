@@ -200,7 +200,7 @@ def _scale_of(amax):
     m, e = torch.frexp(amax.float())
     e = e - 9 + (m > TOP / 512).to(e.dtype)  # TOP = 0.875 * 2^9
     e = torch.where(amax > 0, e, torch.full_like(e, LOWEST)).clamp(min=LOWEST)
-    return torch.ldexp(torch.ones_like(amax, dtype=torch.float32), e)
+    return ((e.to(torch.int32) + 127) << 23).view(torch.float32)
 
 
 def _quantised(x, scale):
@@ -468,10 +468,15 @@ def _exact_head(case, q, k, v, dout):
     return out, dq, dk, dv
 
 
+def _two_to(e):
+    """2^e in 64 bits, exactly (powers and ldexp of torch may be off by a last bit, which decides ties)."""
+    return ((e.to(torch.int64) + 1023) << 52).view(torch.float64)
+
+
 def _exact_e4m3(x):
     """The nearest e4m3 value, ties to even, of |x| <= 448."""
     _, e = torch.frexp(x)
-    step = torch.ldexp(torch.ones_like(x), (e - 1).clamp(min=-6) - 3)
+    step = _two_to((e - 1).clamp(min=-6) - 3)
     return torch.round(x / step) * step
 
 
@@ -489,8 +494,7 @@ def _exact_append(s):
             for name in ("k", "v"):
                 new = s[name][at + done:at + done + count].double().transpose(0, 1)  # [heads, tokens, d]
                 top = new.abs().amax((1, 2))
-                e = torch.ceil(torch.log2(top / TOP)).nan_to_num(neginf=LOWEST).clamp(min=LOWEST)
-                scale = torch.pow(torch.full_like(e, 2.0), e)
+                scale = _two_to(torch.ceil(torch.log2(top / TOP)).nan_to_num(neginf=LOWEST).clamp(min=LOWEST))
                 pool = out[name][page] if name == "k" else out[name][page].transpose(1, 2)  # [heads, tokens, d]
                 if slot:
                     was = out[name + "_scale"][page].clone()
