@@ -203,6 +203,100 @@ int vsa_backward(const vsa_params_t* p, const void* q, const void* k, const void
                  void* dv, void* dgate_c, void* dgate_f, void* workspace, size_t workspace_bytes,
                  void* hip_stream);
 
+/* ---- Windowed attention and its 8-bit cache: models that generate a long clip (or text) piece by piece -------------------
+ *
+ * Positions.  The last query of a sequence stands at its last key: query i of nq is at position i + nk - nq.  Positions are
+ * counted in units of `unit` tokens (the tokens of a frame, or 1).  Key j is visible to position p iff
+ *     floor(j/unit) <= floor(p/unit) + right   and   (floor(j/unit) >= floor(p/unit) - left  or  floor(j/unit) < sinks)
+ * with a negative left or right for no bound: right = 0 is causal (over frames: a frame sees all of itself), `sinks` are the
+ * first units, which stay visible to whoever may look that far ahead.  A query that sees nothing gets a row of zeros, a
+ * log-sum-exp of -inf and no gradient.  Query head h reads key head h / (H / Hkv).
+ *
+ * Tensors are of bf16 or fp16 rows of d (64 or 128) elements; every row is contiguous and 16-byte aligned, batch, token and head
+ * strides are free (in elements, multiples of 8, not negative; those of outputs at least d; token strides at most 2^24).
+ * Dense: B sequences of max_q queries and max_k keys.  Packed: token rows of all sequences one behind the other, sequence b at
+ * rows cu[b] .. cu[b+1] - 1 of total_q (total_k), the batch strides unused.  cu, lens and table are device memory and are not
+ * validated: offsets are clamped to the tensors and to max_q, max_k, so that no access leaves the buffers.  Rows of an output
+ * behind the last sequence are not written.
+ *
+ * Every value of a key row that some query sees must be finite for that row's neighbours to be unaffected: NaN or Inf in a key or
+ * value (in the backward: in any input) may reach all queries of a block of 64 that walk it.  Rows that belong to no sequence, and
+ * cache slots behind the last token, may hold anything.
+ *
+ * These calls allocate nothing, keep nothing from one call to the next, may be captured into a graph, and give the same bits
+ * every time.  (The value range and the workspace rules of the conventions above hold for the calls above only.) */
+#define VSA_DTYPE_BF16 0
+#define VSA_DTYPE_FP16 1
+#define VSA_PAGE_TOKENS 64 /* tokens of a cache page */
+
+typedef struct {
+  int64_t batch, token, head; /* in elements */
+} vsa_strides_t;
+
+typedef struct {
+  int32_t B, H, Hkv, d;       /* sequences, query heads, key heads (a divisor of H), head dimension: 64 or 128 */
+  int32_t max_q, max_k;       /* dense: the lengths; packed: at least the longest                              */
+  int64_t total_q, total_k;   /* packed: rows of the tensors; dense: unused                                    */
+  int32_t unit, left, right, sinks;
+  float softmax_scale;        /* <= 0 selects 1/sqrt(d)                                                        */
+  int32_t dtype;              /* VSA_DTYPE_*                                                                   */
+  vsa_strides_t q, k, v, out; /* forward and backward                                                          */
+  vsa_strides_t dout, dq, dk, dv; /* backward only                                                             */
+} vsa_window_t;
+
+/* Attention of q [.., H, d] over k, v [.., Hkv, d]:  out = softmax(scale q k^T over the visible keys) v.
+ *   cu_q, cu_k   in  int32 [B+1], both (packed) or neither (dense)
+ *   lse          out fp32 [H, rows], rows = total_q (packed) or B*max_q (dense): log-sum-exp of the scaled logits, or NULL */
+int vsa_window_forward(const vsa_window_t* p, const void* q, const void* k, const void* v, const int32_t* cu_q,
+                       const int32_t* cu_k, void* out, float* lse, void* hip_stream);
+
+/* Its gradients.  out and lse as the forward wrote them; dq, dk, dv are written whole (keys that no query sees: zeros), the heads
+ * of a group summed into their key head in fp32.  fp16: dS = P (dP - rowsum(dout out)) must stay below 65504. */
+size_t vsa_window_workspace_bytes(const vsa_window_t* p); /* of the backward; 0 for invalid parameters.  Host-only. */
+int vsa_window_backward(const vsa_window_t* p, const void* q, const void* k, const void* v, const int32_t* cu_q,
+                        const int32_t* cu_k, const void* out, const void* dout, const float* lse, void* dq, void* dk, void* dv,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The cache: `pages` pages of 64 tokens in e4m3 with an fp32 scale per page and key head, K and V apart:
+ *   k_pages  uint8 [pages, Hkv, 64, d]     k_scale  fp32 [pages, Hkv]     key   = value * scale
+ *   v_pages  uint8 [pages, Hkv, d, 64]     v_scale  fp32 [pages, Hkv]     (values transposed: what the product over tokens reads)
+ *   table    int32 [B, max_pages]: the pages of a sequence in order.  Entries that no call of that sequence reaches, and those
+ *            of pages that its window has left, may be anything; an entry outside [0, pages) names nothing: what is appended there
+ *            is dropped, and attention sees no key there.
+ *   lens     int32 [B]: tokens of a sequence in the cache */
+typedef struct {
+  int32_t B, H, Hkv, d;       /* (append: H is not used)                                                       */
+  int32_t max_q;              /* new tokens (append) or queries (attention) a sequence: dense exactly, packed at most */
+  int64_t total_q;            /* packed: rows of the tensors                                                   */
+  int32_t pages, max_pages;
+  int32_t unit, left, right, sinks; /* attention only */
+  float softmax_scale;        /* attention only */
+  int32_t dtype;              /* of q, out, or of k, v */
+  vsa_strides_t q, out;       /* attention */
+  vsa_strides_t k, v;         /* append: the new tokens */
+} vsa_cache_t;
+
+/* New tokens k, v [.., Hkv, d] behind the lens[b] tokens a sequence has.  A page's scale is a power of two, the smallest that
+ * brings its largest value to 448 or less (at least 2^-60; NaN and Inf are not counted and stored as NaN); where the new tokens
+ * need a larger one than the page has, what it holds moves to it.  A page that is appended to must belong to one sequence only,
+ * and not be read by another stream meanwhile.  Tokens beyond max_pages * 64 are dropped.
+ *   cu  in  int32 [B+1] (packed) or NULL (dense: max_q new tokens each) */
+int vsa_cache_append(const vsa_cache_t* p, const void* k, const void* v, const int32_t* cu, const int32_t* lens,
+                     const int32_t* table, void* k_pages, void* v_pages, float* k_scale, float* v_scale, void* hip_stream);
+
+/* Attention of q [.., H, d] over the cache: vsa_window_forward with the keys and values of the first lens[b] tokens (the queries
+ * are the last of them), as the pages stand for them.  Scales must be positive and finite.
+ *   lse  out fp32 [H, rows] or NULL, as in vsa_window_forward */
+size_t vsa_cache_workspace_bytes(const vsa_cache_t* p); /* 0 for invalid parameters.  Host-only. */
+int vsa_cache_attention(const vsa_cache_t* p, const void* q, const int32_t* cu, const int32_t* lens, const int32_t* table,
+                        const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale, void* out, float* lse,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Host-only diagnostic (no GPU, nothing enqueued): replays on the CPU, through the functions the kernels use, how blocks of queries
+ * walk the keys of a sequence of nq queries and nk keys, and blocks of keys its queries, and counts the pairs that a walk misses,
+ * visits twice, masks wrongly or calls unmasked where some pair is not visible.  Returns VSA_OK if there is none. */
+int vsa_host_window_walk(const vsa_window_t* p, int32_t nq, int32_t nk, int64_t* wrong);
+
 /* Host-only diagnostic (no GPU, nothing enqueued): replays on the CPU the index arithmetic the
  * kernels apply to a block-index list -- the clamp of the forward and dQ passes, the skip rule and
  * the capacity of the transposed map, the cutting of long transposed lists into runs with numbered

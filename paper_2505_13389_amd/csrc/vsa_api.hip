@@ -201,18 +201,10 @@ struct Profiler {
 } g_prof;
 
 struct Timed {
-  int slot = -1;
   hipStream_t s;
-  Timed(const char* name, hipStream_t stream) : s(stream) {
-    if (g_prof.on && g_prof.n < g_prof.cap) {
-      slot = g_prof.n++;
-      g_prof.name[slot] = name;
-      (void)hipEventRecord(g_prof.start[slot], s);
-    }
-  }
-  ~Timed() {
-    if (slot >= 0) (void)hipEventRecord(g_prof.stop[slot], s);
-  }
+  int slot;
+  Timed(const char* name, hipStream_t stream) : s(stream), slot(vsa::profile_start(name, stream)) {}
+  ~Timed() { vsa::profile_stop(slot, s); }
 };
 
 #define VSA_TRY(name, expr)                \
@@ -294,6 +286,18 @@ void* static_scratch_of_current_device() {
 }
 
 }  // namespace
+
+// the same recorder for the entry points of window_api.hip
+int vsa::profile_start(const char* name, hipStream_t s) {
+  if (!g_prof.on || g_prof.n >= g_prof.cap) return -1;
+  const int slot = g_prof.n++;
+  g_prof.name[slot] = name;
+  (void)hipEventRecord(g_prof.start[slot], s);
+  return slot;
+}
+void vsa::profile_stop(int slot, hipStream_t s) {
+  if (slot >= 0) (void)hipEventRecord(g_prof.stop[slot], s);
+}
 
 extern "C" {
 

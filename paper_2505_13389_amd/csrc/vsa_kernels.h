@@ -5,6 +5,10 @@
 
 namespace vsa {
 
+// vsa_profile_*: a slot of the recorder (-1: it is off or full), to be closed behind the launch
+int profile_start(const char* name, hipStream_t s);
+void profile_stop(int slot, hipStream_t s);
+
 // `raster` (raster_map or tiled_map): where `out`, `dout` and the gradients lie
 constexpr int kPermuteTensors = 8;  // of one launch, by value
 struct PermuteTensors {

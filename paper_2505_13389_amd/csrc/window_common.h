@@ -1,0 +1,147 @@
+// Windowed attention: what a query sees, where sequences and rows lie, and how a block of queries walks its keys.
+//
+// The last query of a sequence stands at its last key: query i is at position i + nk - nq.  Positions are counted in units
+// of `unit` tokens (a frame, or 1).  Key j is visible to position p iff
+//     j/unit <= p/unit + right   and   (j/unit >= p/unit - left  or  j/unit < sinks)
+// (a negative left or right is no bound), which is j < hi && (j >= lo || j < se) with three numbers a query.  All three
+// never fall from one query to the next, so the first and the last query of a block say what a run of keys is to all of it.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace vsa {
+
+struct WinMask {
+  int unit, left, right, sinks;
+};
+
+struct WinSpan {
+  int lo, hi, se;  // lo <= hi, se <= hi <= nk
+};
+
+__host__ __device__ inline WinSpan win_span(const WinMask& m, int pos, int nk) {
+  long long u = pos;
+  if (m.unit > 1) {
+    const int t = pos / m.unit;
+    u = t - (pos - t * m.unit < 0 ? 1 : 0);
+  }
+  auto clamp = [](long long x, int top) { return (int)(x < 0 ? 0 : x > top ? top : x); };
+  WinSpan s;
+  s.hi = m.right < 0 ? nk : clamp((u + m.right + 1) * m.unit, nk);
+  s.lo = m.left < 0 ? 0 : clamp((u - m.left) * m.unit, s.hi);
+  s.se = clamp((long long)m.sinks * m.unit, s.hi);
+  return s;
+}
+
+// Keys that queries at positions first .. last walk, in pieces of `piece` keys: [0, sink) and then [from, to).  Keys of the
+// second run that a row does not see and of the first behind `sink` are masked.
+struct WinWalk {
+  WinSpan a, z;  // of the first and the last query
+  int sink, from, n_sink, n;  // pieces of the sinks, of both runs
+  int piece;
+  // `align`: the second run begins at a multiple of it
+  __host__ __device__ WinWalk(const WinMask& m, int first, int last, int nk, int piece_, int align) : piece(piece_) {
+    a = win_span(m, first, nk);
+    z = win_span(m, last, nk);
+    from = a.lo / align * align;
+    sink = z.se < from ? z.se : from;
+    n_sink = (sink + piece - 1) / piece;
+    n = n_sink + (z.hi - from + piece - 1) / piece;
+  }
+  __host__ __device__ int begin(int i) const { return i < n_sink ? i * piece : from + (i - n_sink) * piece; }
+  // whether piece i holds keys that some query of the block does not see
+  __host__ __device__ bool masked(int i) const {
+    const int e = begin(i) + piece;
+    if (i < n_sink) return e > a.se || e > sink;
+    return !(e <= a.hi && (e - piece >= z.lo || e <= a.se));
+  }
+  // of one query with span s: the visible keys of piece i are those with j < hi && (j >= lo || j < se)
+  __host__ __device__ WinSpan span_in(int i, const WinSpan& s) const {
+    if (i >= n_sink) return s;
+    const int e = s.se < sink ? s.se : sink;
+    return {e, e, e};
+  }
+};
+
+// Queries that see any of the keys k0 .. k1 - 1 are those of [from, to); key j is seen from position lo up to (not with) hi.
+struct KeySpan {
+  long long lo, hi;
+};
+__host__ __device__ inline KeySpan key_span(const WinMask& m, int j) {
+  const long long u = j / m.unit, far = 1ll << 40;
+  return {m.right < 0 ? -far : (u - m.right) * m.unit, m.left < 0 || u < m.sinks ? far : (u + m.left + 1) * m.unit};
+}
+struct KeyWalk {
+  int from, to, n;  // queries; pieces of `piece` of them
+  long long seen_from, seen_to;  // positions that see all of the keys
+  __host__ __device__ KeyWalk(const WinMask& m, int k0, int k1, int nq, int shift, int piece) {
+    const KeySpan a = key_span(m, k0), z = key_span(m, k1 - 1);
+    auto clamp = [&](long long x) { return (int)(x < 0 ? 0 : x > nq ? nq : x); };
+    from = clamp(a.lo - shift);
+    // (the first keys may be sinks and the others not)
+    const long long edge = (long long)m.sinks * m.unit, last = a.hi > z.hi ? a.hi : z.hi;
+    to = clamp(last - shift);
+    if (to < from) to = from;
+    n = (to - from + piece - 1) / piece;
+    seen_from = z.lo;
+    seen_to = z.hi;  // never falls from key to key behind the sinks; the first key behind them has the least
+    const long long first_other = k0 > edge ? k0 : edge;
+    if (first_other < k1) seen_to = key_span(m, (int)first_other).hi;
+  }
+};
+
+// A tensor of token rows: byte strides of batch, token and head (packed tensors: batch 0).
+struct RowView {
+  const unsigned char* p;
+  long long batch, token, head;
+  __host__ __device__ const unsigned char* row(int b, long long t, int h) const { return p + b * batch + t * token + h * head; }
+  __host__ __device__ unsigned char* out(int b, long long t, int h) const { return const_cast<unsigned char*>(row(b, t, h)); }
+};
+
+// Where the rows of a sequence lie.  Offsets come from device memory and are not trusted: no row leaves [0, total), and no
+// sequence is longer than `most`, for which the launch is made.
+struct WinRows {
+  const int32_t* cu;  // offsets of packed sequences, or null: dense, `most` rows each
+  int most;
+  long long total;
+};
+struct WinSeq {
+  long long row0;  // first row in the tensor (packed) or 0 (dense)
+  int n;
+};
+__host__ __device__ inline WinSeq win_seq(const WinRows& r, int b) {
+  if (!r.cu) return {0, r.most};
+  long long s = r.cu[b], e = r.cu[b + 1];
+  s = s < 0 ? 0 : s > r.total ? r.total : s;
+  const long long top = r.total - s < r.most ? r.total : s + r.most;
+  e = e < s ? s : e > top ? top : e;
+  return {s, (int)(e - s)};
+}
+
+// Workgroup number -> (sequence, item) with `items` of a sequence padded up to a multiple of 8.
+// Workgroups are dealt to the 8 XCDs in turn.  `chunked`: an XCD takes a contiguous run of a sequence's items, so that
+// neighbours (the heads of a group, then the next queries), which read the same keys, find them in one L2; sequences may differ in
+// length, so the runs are of a sequence and not of the launch.  Otherwise in turn, for items of unequal work.
+__device__ __forceinline__ bool win_item(unsigned block, unsigned items, bool chunked, int& b, unsigned& item) {
+  const unsigned padded = (items + 7u) & ~7u;
+  b = (int)(block / padded);
+  const unsigned i = block - (unsigned)b * padded, per = padded >> 3;
+  item = chunked ? (i & 7u) * per + (i >> 3) : i;
+  return item < items;
+}
+inline unsigned win_grid(int B, unsigned items) { return (unsigned)B * ((items + 7u) & ~7u); }
+
+struct WinArgs {
+  WinMask mask;
+  int B, H, Hkv, G;  // G = H / Hkv
+  WinRows rq, rk;
+  RowView q, k, v, o, dout, dq, dk, dv;
+  float* lse;    // [H, lse_rows]
+  float2* stats;  // [H, lse_rows], of the backward: lse in log2 units (+inf for a row that sees nothing), rowsum(dO * O)
+  long long lse_rows;
+  float scale;
+  // row of the statistics of query i of sequence b with first row row0
+  __device__ long long stat(int h, int b, long long row0, int i) const { return h * lse_rows + (rq.cu ? row0 : (long long)b * rq.most) + i; }
+};
+
+}  // namespace vsa

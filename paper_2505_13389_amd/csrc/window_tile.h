@@ -1,0 +1,109 @@
+// Operands and copies of the windowed-attention kernels: both 16-bit types, rows with any stride, and pages of the 8-bit cache.
+#pragma once
+#include "fine_tile.h"
+#include "window_common.h"
+
+namespace vsa {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// Operands are carried as bf16x8 whatever their type: 16 bytes.
+template <bool F16>
+__device__ __forceinline__ f32x16 mm32(bf16x8 a, bf16x8 b, f32x16 c) {
+  if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+template <bool F16>
+__device__ __forceinline__ f32x4 mm16(bf16x8 a, bf16x8 b, f32x4 c) {
+  if constexpr (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// two floats to 16 bits, to the nearest even
+template <bool F16>
+__device__ __forceinline__ uint32_t pack16(float a, float b) {
+  if constexpr (F16) {
+    const f32x2 x = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, f16x2));
+  } else {
+    return pack_bf16(a, b);
+  }
+}
+template <bool F16>
+__device__ __forceinline__ void widen16(uint32_t u, float& a, float& b) {
+  if constexpr (F16) {
+    const f16x2 x = __builtin_bit_cast(f16x2, u);
+    a = (float)x[0], b = (float)x[1];
+  } else {
+    a = bf_lo(u), b = bf_hi(u);
+  }
+}
+template <bool F16>
+__device__ __forceinline__ void widen8(const uint4& u, float* f) {
+  widen16<F16>(u.x, f[0], f[1]);
+  widen16<F16>(u.y, f[2], f[3]);
+  widen16<F16>(u.z, f[4], f[5]);
+  widen16<F16>(u.w, f[6], f[7]);
+}
+
+// eight e4m3 values (8 bytes) to 16 bits: exact, e4m3's values are all bf16 and fp16 values
+template <bool F16>
+__device__ __forceinline__ bf16x8 from_e4m3(uint32_t lo, uint32_t hi) {
+  uint4 u;
+  if constexpr (F16) {
+    u.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false));
+    u.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true));
+    u.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false));
+    u.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
+  } else {
+    u.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
+    u.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
+    u.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
+    u.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
+  }
+  return __builtin_bit_cast(bf16x8, u);
+}
+
+// 64 lanes x 16 bytes, global -> 1 KiB of LDS at `lds`.  The base may have come out of a vector register right before, which
+// takes 5 wait states; M0 takes one.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void win_copy16(const void* base, unsigned voff, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff), "s"(base), "s"(lds) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+template <int N>
+__device__ __forceinline__ void win_wait() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Copies of 32 rows with any stride by one wavefront: instruction c fills LDS rows c*RPI .., swizzled on the source side.
+template <int D>
+struct RowCopy {
+  using TL = Tile<D>;
+  static constexpr int NC = 32 / TL::RPI;
+  unsigned off[NC];
+  __device__ __forceinline__ unsigned at(int c, int lane, unsigned stride, int last) const {
+    const int x = c * TL::RPI + lane / TL::CPR, pc = lane % TL::CPR;
+    return (unsigned)min(x, last) * stride + ((pc ^ TL::swz(x)) << 4);
+  }
+  __device__ __forceinline__ void init(int lane, unsigned stride) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) off[c] = at(c, lane, stride, 31);
+  }
+  __device__ __forceinline__ void piece(const void* base, unsigned lds, int c) const { win_copy16(base, off[c], lds + (unsigned)c * 1024u); }
+  // `have` rows are there: the last of them stands for those behind it
+  __device__ __forceinline__ void all(const void* base, unsigned lds, int lane, unsigned stride, int have) const {
+    if (have >= 32) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) piece(base, lds, c);
+    } else {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) win_copy16(base, at(c, lane, stride, have - 1), lds + (unsigned)c * 1024u);
+    }
+  }
+};
+
+}  // namespace vsa

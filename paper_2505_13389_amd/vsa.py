@@ -27,7 +27,8 @@ STATUS = {0: "VSA_OK", -1: "VSA_ERR_NULL", -2: "VSA_ERR_BAD_ARG", -3: "VSA_ERR_U
 EXPORTS = ["vsa_padded_tokens", "vsa_workspace_bytes", "vsa_tile_permute", "vsa_tile_permute_many", "vsa_forward", "vsa_backward",
            "vsa_status_string", "vsa_profile_begin", "vsa_profile_count", "vsa_profile_name", "vsa_profile_ms",
            "vsa_profile_end", "vsa_bench_mfma_rate", "vsa_forward_static", "vsa_static_scratch_bytes", "vsa_host_replay_lists",
-           "vsa_host_routes"]
+           "vsa_host_routes", "vsa_window_forward", "vsa_window_workspace_bytes", "vsa_window_backward", "vsa_cache_append",
+           "vsa_cache_workspace_bytes", "vsa_cache_attention", "vsa_host_window_walk"]
 
 
 class VsaParams(C.Structure):
@@ -74,6 +75,16 @@ def lib():
         L.vsa_host_routes.restype = C.c_int
         L.vsa_backward.argtypes = [C.POINTER(VsaParams)] + [vp] * 17 + [C.c_size_t, vp]
         L.vsa_backward.restype = C.c_int
+        # (parameters of these: the structures of window.py)
+        L.vsa_window_forward.argtypes = [vp] * 9
+        L.vsa_window_workspace_bytes.argtypes = [vp]
+        L.vsa_window_workspace_bytes.restype = C.c_size_t
+        L.vsa_window_backward.argtypes = [vp] * 13 + [C.c_size_t, vp]
+        L.vsa_cache_append.argtypes = [vp] * 11
+        L.vsa_cache_workspace_bytes.argtypes = [vp]
+        L.vsa_cache_workspace_bytes.restype = C.c_size_t
+        L.vsa_cache_attention.argtypes = [vp] * 12 + [C.c_size_t, vp]
+        L.vsa_host_window_walk.argtypes = [vp, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]
         L.vsa_bench_mfma_rate.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.POINTER(C.c_double), C.c_void_p]
         L.vsa_profile_begin.argtypes = [C.c_int]
         L.vsa_profile_name.argtypes = [C.c_int]
