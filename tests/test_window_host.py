@@ -157,7 +157,7 @@ def test_leaves_that_another_graph_holds_are_refused(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream)
     q, k = torch.zeros(3, requires_grad=True), torch.zeros(3, requires_grad=True)
     plain = torch.zeros(3)
-    nodes = autograd._refuse_held_leaves(q, k, plain, q * 2)
+    nodes = autograd._refuse_held_leaves(q, k, plain, torch.zeros(3, requires_grad=True) * 2)  # (not a leaf)
     assert len(nodes) == 2
     alive = q * 2  # of the same capture: marked with its stream
     assert len(autograd._refuse_held_leaves(q, k, plain)) == 2
