@@ -78,8 +78,9 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, unsigned it
   const WinSeq sq = win_seq(a.rq, b), sk = win_seq(a.rk, b);
   const int r0 = qb * 64, rows = min(64, sq.n - r0);
   if (rows <= 0) return;
-  const int nk = sk.n, shift = nk - sq.n;
-  const WinWalk walk(a.mask, r0 + shift, r0 + rows - 1 + shift, nk, 32, 1);
+  const int nk = __builtin_amdgcn_readfirstlane(sk.n), shift = nk - sq.n;
+  WinWalk walk(a.mask, r0 + shift, r0 + rows - 1 + shift, nk, 32, 1);
+  walk.uniform();
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, h = lane >> 5;
   const int nu = walk.n > wave ? (walk.n - wave + NW - 1) / NW : 0;
@@ -114,8 +115,8 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, unsigned it
   vc.init(lane, vstride);
   auto copy = [&](int u, int stage) {
     const int at = walk.begin(wave + NW * u);
-    kc.all(kb + (long long)at * kstride, lds0 + stage * HALF, lane, kstride, nk - at);
-    vc.all(vb + (long long)at * vstride, lds0 + (2 + stage) * HALF, lane, vstride, nk - at);
+    kc.all(kb + (long long)at * kstride, lds0 + stage * HALF, lane, nk - at);
+    vc.all(vb + (long long)at * vstride, lds0 + (2 + stage) * HALF, lane, nk - at);
   };
   f32x16 acc[DVB][2], zero16;
 #pragma unroll
@@ -242,8 +243,8 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, unsigned i
     const unsigned char* qb = (const unsigned char*)uniform_ptr(a.q.row(b, sq.row0 + at, hq));
     const unsigned char* db = (const unsigned char*)uniform_ptr(a.dout.row(b, sq.row0 + at, hq));
     const void* sb = uniform_ptr(a.stats + a.stat(hq, b, sq.row0, at));
-    qc.all(qb, lds0 + stage * HALF, lane, qstride, have);
-    dc.all(db, lds0 + (2 + stage) * HALF, lane, dstride, have);
+    qc.all(qb, lds0 + stage * HALF, lane, have);
+    dc.all(db, lds0 + (2 + stage) * HALF, lane, have);
     lds_dma4<4>(sb, (unsigned)min(lane >> 1, have - 1) * 8u + (lane & 1) * 4u, stat0 + stage * 256u);
   };
   f32x16 dk[DVB][KT], dv[DVB][KT], zero16;

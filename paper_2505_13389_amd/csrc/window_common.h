@@ -49,6 +49,16 @@ struct WinWalk {
     n = n_sink + (z.hi - from + piece - 1) / piece;
   }
   __host__ __device__ int begin(int i) const { return i < n_sink ? i * piece : from + (i - n_sink) * piece; }
+#if defined(__HIP_DEVICE_COMPILE__)
+  // (equal in all lanes: into scalar registers, where the arithmetic that led here has not put them)
+  __device__ __forceinline__ void uniform() {
+    int* const all[] = {&a.lo, &a.hi, &a.se, &z.lo, &z.hi, &z.se, &sink, &from, &n_sink, &n};
+#pragma unroll
+    for (int i = 0; i < 10; ++i) *all[i] = __builtin_amdgcn_readfirstlane(*all[i]);
+  }
+#else
+  __host__ __device__ void uniform() {}
+#endif
   // whether piece i holds keys that some query of the block does not see
   __host__ __device__ bool masked(int i) const {
     const int e = begin(i) + piece;

@@ -9,6 +9,10 @@
 // PAGED: K and V come from the pages of the 8-bit cache, as bytes, and are widened as operands.  Rows of the tile are keys in an
 // order that puts a lane's 16 values of S^T at consecutive keys, and a contraction step pair of K at 16 consecutive bytes:
 // every LDS read is 16 bytes.  K's scale goes into the softmax's factor, V's into its exponent and reference: see k_cache_token.
+#include <type_traits>
+
+#include "ticks.h"
+#include "unit_stream.h"
 #include "window_kernels.h"
 #include "window_tile.h"
 
@@ -67,11 +71,67 @@ struct PageCopy {
   }
 };
 
+// What lies behind which matrix instruction of a unit (see ticks.h): S of the next unit, then PV.  The softmax of a unit, in
+// operations, is done from the second instruction of the PV phase before it to the last but one of the next S phase.
+template <int D, bool PAGED>
+struct WinTicks : TickCycles<D / 2> {  // (two units)
+  using Table = TickCycles<D / 2>;
+  using typename Table::Work;
+  using Table::cycles;
+  using Table::T;
+  static constexpr int KS = D / 16, PH = 2 * KS, U = T / 2;  // contraction steps of S (and operands of V); matrix instructions of a phase, of a unit
+  static constexpr int NC = PAGED ? D / 32 : KS;             // copies of a unit's K, or V
+  static constexpr int kEvery = PH / NC < 4 ? PH / NC : 4;   // a copy behind every so many
+  static constexpr int kAhead = D == 128 ? 4 : 2;            // operands are read so many steps ahead
+  static constexpr int kOps = 112;
+  Work w[kOps] = {};
+  int ahead[T + 1] = {};
+  static constexpr int in_pv(int j) { return PH + j; }
+  static constexpr int in_s(int j) { return U + j; }
+  constexpr WinTicks() {
+    for (int t = 0; t < T; ++t) {
+      const int u = t % U, j = u % PH;
+      if (j % kEvery == 0 && j / kEvery < NC) cycles[t] += Table::kCopy + (j == 0 ? 5 * Table::kScalar : 0);
+      if (j % 2 == 0) cycles[t] += Table::kRead;               // (operands: two reads of V's, one of K's, of either one in pages)
+      if (j % 2 == 1 && u >= PH && !PAGED) cycles[t] += Table::kRead;
+      if (PAGED) cycles[t] += 2 * 5;                           // widening
+      if (u < PH && j == PH - 2) cycles[t] += 38;              // the check of the references
+      if (u < PH && (j == 1 || j == 3)) cycles[t] += 5 * Table::kScalar;  // where the next unit lies
+    }
+    int n = 0;
+    w[n++] = {Table::MUL, 0, 0};
+    w[n++] = {Table::MUL, 0, 1};
+    for (int g = 0; g < 17; ++g) {
+      if (g < 16) w[n++] = {Table::EXP, g, 0};
+      if (g < 15) w[n++] = {Table::MUL, g + 1, 0};
+      if (g < 15) w[n++] = {Table::MUL, g + 1, 1};
+      if (g < 16) w[n++] = {Table::EXP, g, 1};
+      if (g > 0) w[n++] = {Table::ADD, g - 1, 0};
+      if (g > 0) w[n++] = {Table::CVT, g - 1, 0};
+      if (g > 0) w[n++] = {Table::ADD, g - 1, 1};
+    }
+    this->deal(ahead, w, kOps, in_pv(1), in_s(PH - 1));
+  }
+  constexpr bool in_order() const { return ahead[in_pv(1)] == 0 && ahead[in_s(PH - 1)] == kOps && this->ordered(w, kOps); }
+};
+static_assert(WinTicks<128, false>().in_order() && WinTicks<64, false>().in_order() && WinTicks<128, true>().in_order() && WinTicks<64, true>().in_order(),
+              "operations of the softmax");
+
+// O of d = 128 lives in the accumulation registers (256 + 256 registers a wavefront, see mfma_a)
+template <int D, bool F16>
+__device__ __forceinline__ void mm_o(f32x16& acc, bf16x8 a, bf16x8 b) {
+  if constexpr (D == 64) acc = mm32<F16>(a, b, acc);
+  else if constexpr (F16) asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+  else mfma_a(acc, a, b);
+}
+
 template <int D, bool F16, int NW, bool PAGED>
-__global__ __launch_bounds__(64 * NW, D == 128 ? 1 : 2) void k_window_fwd(WinArgs a, CacheArgs cache, unsigned items, int nqb, int chunked) {
+__global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs cache, unsigned items, int nqb, int chunked) {
   using TL = Tile<D>;
-  constexpr int KS = D / 16, DVB = D / 32, HALF = 32 * D * 2, STAGE = PAGED ? HALF / 2 : HALF;
-  constexpr int NC = PAGED ? PageCopy<D>::NC : RowCopy<D>::NC;
+  using TK = WinTicks<D, PAGED>;
+  constexpr TK ticks;
+  constexpr int KS = D / 16, DVB = D / 32, PH = 2 * KS, HALF = 32 * D * 2, STAGE = PAGED ? HALF / 2 : HALF, NC = TK::NC, kAhead = TK::kAhead, kEvery = TK::kEvery;
+  static_assert(NC == (PAGED ? PageCopy<D>::NC : RowCopy<D>::NC) && (NC - 1) * kEvery < PH, "copies of a phase");
   __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * 4 * HALF];
   __shared__ float ml[NW * 64 * 2];
 
@@ -86,8 +146,9 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : 2) void k_window_fwd(WinArg
   WinSeq sk = {0, 0};
   if constexpr (PAGED) sk.n = max(0, min(cache.lens[b], cache.max_pages * kPage));
   else sk = win_seq(a.rk, b);
-  const int nk = sk.n, shift = nk - sq.n;
-  const WinWalk walk(a.mask, r0 + shift, r0 + rows - 1 + shift, nk, 32, PAGED ? 32 : 1);
+  const int nk = __builtin_amdgcn_readfirstlane(sk.n), shift = nk - sq.n;
+  WinWalk walk(a.mask, r0 + shift, r0 + rows - 1 + shift, nk, 32, PAGED ? 32 : 1);
+  walk.uniform();
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, h = lane >> 5;
@@ -109,7 +170,6 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : 2) void k_window_fwd(WinArg
 
   const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem)) + (unsigned)wave * (4 * HALF);
   unsigned char* const mine = smem + wave * (4 * HALF);
-  const unsigned kstride = (unsigned)a.k.token, vstride = (unsigned)a.v.token;
   const unsigned char *kb = nullptr, *vb = nullptr;
   RowCopy<D> kc, vc;
   PageCopy<D> pc;
@@ -120,171 +180,373 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : 2) void k_window_fwd(WinArg
   } else {
     kb = (const unsigned char*)uniform_ptr(a.k.row(b, sk.row0, hk));
     vb = (const unsigned char*)uniform_ptr(a.v.row(b, sk.row0, hk));
-    kc.init(lane, kstride);
-    vc.init(lane, vstride);
+    kc.init(lane, (unsigned)a.k.token);
+    vc.init(lane, (unsigned)a.v.token);
   }
+  // A unit of the wavefront's walk, and where its rows lie.  (Units behind the last one are that one again: their copies are
+  // made, so that the waits can count, and not used.)
   struct U {
-    int a;            // first key
+    int a;                           // first key
     bool masked;
-    int page;         // PAGED: its page, or -1
-    float sk, lv;     // PAGED: scale of K, log2 of the scale of V
+    const unsigned char *k, *v;
+    float f, lv;                     // of the softmax: P' = exp2(f S + lv - ref)
   };
+  const float sl2 = a.scale * kLog2e;
   auto unit = [&](int u) {
     const int i = wave + NW * min(u, nu - 1);
-    U x = {walk.begin(i), walk.masked(i), 0, 1.f, 0.f};
+    U x;
+    x.a = walk.begin(i);
+    x.masked = walk.masked(i);
+    x.f = sl2, x.lv = 0.f;
     if constexpr (PAGED) {
       const int e = x.a / kPage;
       pages.want(e);
-      x.page = pages.page_id(e);
-      x.masked |= x.page < 0;
-      x.sk = pages.scale_k(e);
+      const int id = pages.page_id(e);
+      x.masked |= id < 0;
+      x.f = sl2 * pages.scale_k(e);
       x.lv = fast_log2(pages.scale_v(e));
+      const long long at = ((long long)max(id, 0) * a.Hkv + hk) * (kPage * D);
+      x.k = cache.k + at + (x.a & 32) * D;
+      x.v = cache.v + at + (x.a & 32);
+      x.a = id < 0 ? nk : x.a;  // (no key of it is visible)
+    } else {
+      x.k = kb + (long long)x.a * kc.stride;
+      x.v = vb + (long long)x.a * vc.stride;
     }
     return x;
   };
-  auto page_base = [&](const uint8_t* pool, const U& x, int bytes) {
-    return (const unsigned char*)uniform_ptr(pool + ((long long)max(x.page, 0) * a.Hkv + hk) * (kPage * D) + bytes);
-  };
-  auto copy_k = [&](const U& x, int stage) {
+  // copies of a unit's K into stage 0 or 1, V into 2 or 3
+  auto copy_all = [&](const U& x, bool of_v, int stage) {
+    const unsigned lds = lds0 + stage * STAGE;
     if constexpr (PAGED) {
-      const unsigned char* base = page_base(cache.k, x, (x.a & 32) * D);
 #pragma unroll
-      for (int c = 0; c < NC; ++c) win_copy16(base, pc.ko[c], lds0 + stage * STAGE + c * 1024);
+      for (int c = 0; c < NC; ++c) win_copy16(of_v ? x.v : x.k, of_v ? pc.vo[c] : pc.ko[c], lds + c * 1024);
     } else {
-      kc.all(kb + (long long)x.a * kstride, lds0 + stage * STAGE, lane, kstride, nk - x.a);
+      int l = lane;
+      asm volatile("" : "+v"(l));  // (nothing of this is kept in registers through the walk)
+      if (of_v) vc.all(x.v, lds, l, nk - x.a);
+      else kc.all(x.k, lds, l, nk - x.a);
     }
   };
-  auto copy_v = [&](const U& x, int stage) {
-    if constexpr (PAGED) {
-      const unsigned char* base = page_base(cache.v, x, x.a & 32);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) win_copy16(base, pc.vo[c], lds0 + (2 + stage) * STAGE + c * 1024);
-    } else {
-      vc.all(vb + (long long)x.a * vstride, lds0 + (2 + stage) * STAGE, lane, vstride, nk - x.a);
-    }
+  auto copy_aim = [&](bool of_v, int stage, int c) {
+    if constexpr (PAGED) set_m0_ahead(lds0 + stage * STAGE + c * 1024);
+    else (of_v ? vc : kc).aim(lds0 + stage * STAGE, c);
+    __builtin_amdgcn_sched_barrier(0);  // (the matrix instruction between this and the copy stays between them)
+  };
+  auto copy_piece = [&](const U& x, bool of_v, int c) {
+    if constexpr (PAGED) lds_dma16_at<0>(of_v ? x.v : x.k, of_v ? pc.vo[c] : pc.ko[c]);
+    else if (of_v) vc.piece(x.v, c);
+    else kc.piece(x.k, c);
   };
 
-  f32x16 o[DVB][2], s[2];
+  f32x16 o[DVB][2];
+  float nil = 0.f;
+  asm volatile("" : "+v"(nil));
 #pragma unroll
   for (int x = 0; x < DVB; ++x)
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[x][t][i] = 0.f;
+      for (int i = 0; i < 16; ++i) o[x][t][i] = nil;
+  auto pin_o = [](f32x16& acc) {
+    if (D == 128) asm volatile("" : "+a"(acc));
+    else asm volatile("" : "+v"(acc));
+  };
+#pragma unroll
+  for (int x = 0; x < DVB; ++x) pin_o(o[x][0]), pin_o(o[x][1]);
+
   float ref[2] = {kUnset, kUnset}, lsum[2] = {0.f, 0.f};
-  bool have = false;  // every column has a reference
-  const float sl2 = a.scale * kLog2e;
+  float ta[2] = {0.f, 0.f}, tb[2] = {0.f, 0.f};  // a lane's sums of a unit, even and odd values
+  uint4 pb[2][2];                                // P^T as operands: [query half][contraction step]
   f32x16 zero16;
 #pragma unroll
   for (int i = 0; i < 16; ++i) zero16[i] = 0.f;
 
-  if (nu > 0) {
-    U cur = unit(0);
-    copy_k(cur, 0);
-    copy_v(cur, 0);
-    for (int u = 0; u < nu; ++u) {
-      const int par = u & 1;
-      const U next = unit(u + 1);
-      if (u + 1 < nu) {
-        copy_k(next, 1 - par);
-        copy_v(next, 1 - par);
-        win_wait<2 * NC>();
-      } else {
-        win_wait<0>();
+  auto put = [](uint4& u4, int w, uint32_t x) {
+    if (w == 0) u4.x = x;
+    if (w == 1) u4.y = x;
+    if (w == 2) u4.z = x;
+    if (w == 3) u4.w = x;
+  };
+  // Item `it` of 16 of a unit's softmax: two values of one query half, the first eight of contraction step 0
+  float xf[2][2] = {}, xe[2][2] = {};
+  auto p_fma = [&](const f32x16 (&S)[2], int it, int i, float f, const float* sub) {
+    const int t = (it >> 2) & 1, e = 8 * (it >> 3) + 2 * (it & 3);
+    xf[it & 1][i] = fmaf(S[t][e + i], f, -sub[t]);
+    asm volatile("" : : "v"(xf[it & 1][i]));  // (pure arithmetic has no place of its own in the order: tie it to this one)
+  };
+  auto p_exp = [&](int it, int i) {
+    xe[it & 1][i] = fast_exp2(xf[it & 1][i]);
+    asm volatile("" : : "v"(xe[it & 1][i]));
+  };
+  auto p_sum = [&](int it, int i) {
+    float& t = (i ? tb : ta)[(it >> 2) & 1];
+    const float x = xe[it & 1][i];
+    t = (it & 11) == 0 ? x : t + x;
+    asm volatile("" : : "v"(t));
+  };
+  auto p_convert = [&](int it) {
+    const uint32_t pp = pack16<F16>(xe[it & 1][0], xe[it & 1][1]);
+    put(pb[(it >> 2) & 1][it >> 3], it & 3, pp);
+    asm volatile("" : : "v"(pp));
+  };
+  auto p_ops = [&](const f32x16 (&S)[2], auto from, auto to, float f, const float* sub) {
+    in_steps<decltype(to)::value - decltype(from)::value>([&](auto number) {
+      constexpr typename TK::Work w = ticks.w[decltype(from)::value + decltype(number)::value];
+      if constexpr (w.op == TK::MUL) p_fma(S, w.item, w.i, f, sub);
+      if constexpr (w.op == TK::EXP) p_exp(w.item, w.i);
+      if constexpr (w.op == TK::ADD) p_sum(w.item, w.i);
+      if constexpr (w.op == TK::CVT) p_convert(w.item);
+    });
+  };
+  auto unit_max = [&](const f32x16& S) {
+    float m = fmaxf(fmaxf(S[0], S[1]), S[2]);
+#pragma unroll
+    for (int i = 3; i < 15; i += 2) m = fmaxf(fmaxf(m, S[i]), S[i + 1]);
+    return max_across_halves(fmaxf(m, S[15]));
+  };
+  auto hide = [&](f32x16 (&S)[2], const U& x, int u) {  // what a query does not see
+    int first = PAGED ? 16 * h : 4 * h;
+    asm volatile("" : "+v"(first));
+    first += x.a;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const WinSpan w = walk.span_in(wave + NW * u, span[t]);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = first + (PAGED ? i : 8 * (i >> 2) + (i & 3));
+        S[t][i] = key < w.hi && (key >= w.lo || key < w.se) ? S[t][i] : -INFINITY;
       }
-      const unsigned char *ks = mine + par * STAGE, *vs = mine + (2 + par) * STAGE;
-      if (PAGED && cur.a + 32 > nk) {  // values behind the last token may be anything: zero
-        const int live = nk - cur.a;
-#pragma unroll
-        for (int dv = lane; dv < D; dv += 64) {
-          unsigned* p = (unsigned*)(vs + dv * 32);
-          for (int w = 0; w < 8; ++w) {
-            const int key = ((w >> 2) ^ ((dv >> 3) & 1)) * 16 + (w & 3) * 4, keep = min(4, max(0, live - key));
-            p[w] = keep == 4 ? p[w] : p[w] & ((1u << (8 * keep)) - 1u);
-          }
-        }
-        __builtin_amdgcn_wave_barrier();
-      }
-      // S^T
-#pragma unroll
-      for (int st = 0; st < KS; ++st) {
-        bf16x8 ka;
-        if constexpr (PAGED) {
-          const uint4 raw = PageCopy<D>::k_at(ks, lane, st >> 1);
-          ka = st & 1 ? from_e4m3<F16>(raw.z, raw.w) : from_e4m3<F16>(raw.x, raw.y);
-        } else {
-          ka = TL::rowmajor_at(ks, TL::rowmajor_lane(0, lane), st);
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) s[t] = mm32<F16>(ka, qreg[t][st], st == 0 ? zero16 : s[t]);
-      }
-      const float f = sl2 * cur.sk;
-      if (cur.masked) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const WinSpan w = walk.span_in(wave + NW * u, span[t]);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = cur.a + (PAGED ? 16 * h + i : 8 * (i >> 2) + 4 * h + (i & 3));
-            const bool see = key < w.hi && (key >= w.lo || key < w.se) && (!PAGED || cur.page >= 0);
-            s[t][i] = see ? s[t][i] : -INFINITY;
-          }
-        }
-      }
-      // P^T: the reference is the running maximum
-      uint32_t p[2][8];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        float m = s[t][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) m = fmaxf(m, s[t][i]);
-        m = fmaxf(fmaf(max_across_halves(m), f, cur.lv), ref[t]);
-        if (__any(m > ref[t])) {
-          const float alpha = fast_exp2(ref[t] - m);
-          lsum[t] *= alpha;
-#pragma unroll
-          for (int x = 0; x < DVB; ++x)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[x][t][i] *= alpha;
-          ref[t] = m;
-        }
-        float e[16], sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          e[i] = fast_exp2(fmaf(s[t][i], f, cur.lv - ref[t]));
-          sum += e[i];
-        }
-        lsum[t] += PAGED ? sum * fast_exp2(-cur.lv) : sum;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[t][i] = pack16<F16>(e[2 * i], e[2 * i + 1]);
-      }
-      // O^T
-#pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        bf16x8 pop[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) pop[t] = __builtin_bit_cast(bf16x8, make_uint4(p[t][4 * st], p[t][4 * st + 1], p[t][4 * st + 2], p[t][4 * st + 3]));
-#pragma unroll
-        for (int x = 0; x < DVB; ++x) {
-          bf16x8 va;
-          if constexpr (PAGED) {
-            const uint4 raw = PageCopy<D>::v_at(vs, lane, x);
-            va = st ? from_e4m3<F16>(raw.z, raw.w) : from_e4m3<F16>(raw.x, raw.y);
-          } else {
-            int b0, b1;
-            TL::transposed_lane(0, lane, b0, b1);
-            va = TL::transposed_at(vs, b0, b1, st, x);
-          }
-#pragma unroll
-          for (int t = 0; t < 2; ++t) o[x][t] = mm32<F16>(va, pop[t], o[x][t]);
-        }
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // every read of the stages is over: they may be filled again
-      __builtin_amdgcn_sched_barrier(0);
-      cur = next;
     }
+  };
+  auto clear_tail = [&](const U& x, int stage) {  // values behind the last token may be anything: zero
+    const int live = nk - x.a;
+    for (int dv = lane; dv < D; dv += 64) {
+      unsigned* p = (unsigned*)(mine + stage * STAGE + dv * 32);
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        const int key = ((w >> 2) ^ ((dv >> 3) & 1)) * 16 + (w & 3) * 4, keep = min(4, max(0, live - key));
+        p[w] = keep == 4 ? p[w] : p[w] & ((1u << (8 * keep)) - 1u);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  };
+
+  const int lane_a = TL::rowmajor_lane(0, lane);
+  int lane_b0, lane_b1;
+  TL::transposed_lane(0, lane, lane_b0, lane_b1);
+  // operand reads.  K: step s; of pages two steps a read.  V: operand i = (contraction step i / DVB, tile i % DVB), two reads; of
+  // pages one for both steps of a tile.
+  constexpr int NK = PAGED ? KS / 2 : KS, NV = PAGED ? DVB : KS;  // reads (V of rows: pairs of them)
+  struct Row8 {
+    bf16x8 x;
+  };
+  using KRaw = std::conditional_t<PAGED, uint4, bf16x8>;
+  using VRaw = std::conditional_t<PAGED, uint4, bf16x8>;
+  auto read_k = [&](int stage, int i) -> KRaw {
+    if constexpr (PAGED) return PageCopy<D>::k_at(mine + stage * STAGE, lane, i);
+    else return TL::rowmajor_at(mine + stage * STAGE, lane_a, i);
+  };
+  auto read_v = [&](int stage, int i) -> VRaw {
+    if constexpr (PAGED) return PageCopy<D>::v_at(mine + stage * STAGE, lane, i);
+    else return TL::transposed_at(mine + stage * STAGE, lane_b0, lane_b1, i / DVB, i % DVB);
+  };
+  auto k_op = [&](const KRaw& r, int s) -> bf16x8 {
+    if constexpr (PAGED) return s & 1 ? from_e4m3<F16>(r.z, r.w) : from_e4m3<F16>(r.x, r.y);
+    else return r;
+  };
+  auto v_op = [&](const VRaw& r, int st) -> bf16x8 {
+    if constexpr (PAGED) return st ? from_e4m3<F16>(r.z, r.w) : from_e4m3<F16>(r.x, r.y);
+    else return r;
+  };
+
+  f32x16 s0[2], s1[2];
+  constexpr int kKeep = PAGED ? kAhead / 2 : kAhead;  // K reads of a unit's first steps, made during the phase before
+  KRaw kcur[kKeep];
+  U cur = {}, n1 = {}, n2 = {};
+  if (nu > 0) {
+    cur = unit(0), n1 = unit(1), n2 = unit(2);
+    copy_all(cur, false, 0);
+    copy_all(n1, false, 1);
+    copy_all(cur, true, 2);
+    win_wait<2 * NC>();  // K of the first unit
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const bf16x8 ka = k_op(read_k(0, PAGED ? s / 2 : s), s);
+      s0[0] = mm32<F16>(ka, qreg[0][s], s == 0 ? zero16 : s0[0]);
+      s0[1] = mm32<F16>(ka, qreg[1][s], s == 0 ? zero16 : s0[1]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    copy_all(n2, false, 0);
+    if (cur.masked) hide(s0, cur, 0);
+    win_wait<2 * NC>();  // K of the second (newer: V of the first, K of the third)
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) kcur[i] = read_k(1, i);
+    // the first reference; a column of which nothing is visible yet has none, and any sum of it is above the bound
+#pragma unroll
+    for (int t = 0; t < 2; ++t) ref[t] = fmaxf(fmaf(unit_max(s0[t]), cur.f, cur.lv), kUnset);
+    const float sub[2] = {ref[0] - cur.lv, ref[1] - cur.lv};
+    p_ops(s0, std::integral_constant<int, 0>{}, std::integral_constant<int, ticks.ahead[TK::U]>{}, cur.f, sub);
   }
-  (void)have;
+
+  // Unit u, whose S is there: P(u) while S(u + 1) is multiplied into T, then PV(u) while P(u + 1) begins.  K(u + 1) has landed, K(u + 2) and
+  // V(u) are on their way; V(u + 1) is requested during the first phase, K(u + 3) during the second.
+  // KIND 2: copies piece by piece; 1: at once (rows that are not there are among them); 0: u is the last unit.
+  auto body = [&](auto kind_tag, auto par_tag, f32x16 (&S)[2], f32x16 (&T)[2], int u) {
+    constexpr int KIND = decltype(kind_tag)::value;
+    constexpr bool more = KIND > 0;
+    constexpr int par = decltype(par_tag)::value;
+    constexpr int kn = 1 - par, vn = 3 - par, vc_ = 2 + par;  // stages: K(u + 1) and then K(u + 3), V(u + 1), V(u)
+    KRaw kr[NK];
+    VRaw vr[NV];
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) kr[i] = kcur[i];
+    const float sub[2] = {ref[0] - cur.lv, ref[1] - cur.lv};
+    U n3 = {};
+    if (KIND == 1) copy_all(n1, true, vn);
+    bf16x8 kop;
+    __builtin_amdgcn_sched_barrier(0);
+    in_steps<PH>([&](auto number) {
+      constexpr int j = decltype(number)::value, s = j >> 1;
+      constexpr bool copies = KIND == 2 && j % kEvery == 0 && j / kEvery < NC;
+      if (copies) copy_aim(true, vn, j / kEvery);
+      if (j % 2 == 0 && more) kop = k_op(kr[PAGED ? s / 2 : s], s);
+      if (more) T[j & 1] = mm32<F16>(kop, qreg[j & 1][s], s == 0 ? zero16 : T[j & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (copies) copy_piece(n1, true, j / kEvery);
+      if (j == PH - 2 * kAhead) {  // V(u) has landed; newer: K(u + 2) and what has been requested of V(u + 1)
+        constexpr int part = (PH - 2 * kAhead) / kEvery + 1 < NC ? (PH - 2 * kAhead) / kEvery + 1 : NC;
+        if constexpr (more) win_wait<NC + (KIND == 2 ? part : NC)>();
+        else win_wait<NC>();
+        if (PAGED && cur.a + 32 > nk) clear_tail(cur, vc_);
+      }
+      // operands kAhead steps further on
+      if constexpr (j % 2 == 0) {
+        constexpr int to = s + kAhead;
+        if constexpr (to < KS) {
+          if constexpr (more && !(PAGED && to % 2)) kr[PAGED ? to / 2 : to] = read_k(kn, PAGED ? to / 2 : to);
+        } else if constexpr (to - KS < NV) {
+          vr[to - KS] = read_v(vc_, to - KS);
+        }
+      }
+      if (j == 1 && more) n3 = unit(u + 3);
+      p_ops(S, std::integral_constant<int, ticks.ahead[TK::in_s(j)]>{}, std::integral_constant<int, ticks.ahead[TK::in_s(j + 1)]>{}, cur.f, sub);
+      __builtin_amdgcn_sched_barrier(0);
+      if (j == PH - 2) {
+        // A column's reference stays unless one of its two lanes sums 16 values to more than kMostSum (infinity: it has none yet).
+        const float tsum[2] = {ta[0] + tb[0], ta[1] + tb[1]};
+        const float out = PAGED ? fast_exp2(-cur.lv) : 1.f;
+        float add[2] = {tsum[0], tsum[1]};
+        if (__builtin_expect(__any(!(fmaxf(tsum[0], tsum[1]) <= kMostSum)), 0)) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const bool moves = !(max_across_halves(tsum[t]) <= kMostSum);
+            if (!__any(moves)) continue;
+            const float to = fmaxf(fmaf(unit_max(S[t]), cur.f, cur.lv), ref[t]), next = moves ? to : ref[t];
+            const float alpha = fast_exp2(ref[t] - next);
+            lsum[t] *= alpha;
+#pragma unroll
+            for (int x = 0; x < DVB; ++x) {
+              pin_o(o[x][t]);  // (moved to ordinary registers from here on and not before the branch)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[x][t][i] *= alpha;
+              pin_o(o[x][t]);
+              __builtin_amdgcn_sched_barrier(0);  // (one block of O in ordinary registers at a time)
+            }
+            ref[t] = next;
+            const float now[2] = {ref[0] - cur.lv, ref[1] - cur.lv};
+#pragma unroll
+            for (int st = 0; st < 2; ++st)
+#pragma unroll
+              for (int w = 0; w < 4; ++w) {
+                const int it = 8 * st + 4 * t + w;
+                for (int i = 0; i < 2; ++i) {
+                  p_fma(S, it, i, cur.f, now);
+                  p_exp(it, i);
+                  p_sum(it, i);
+                }
+                p_convert(it);
+              }
+            add[t] = ta[t] + tb[t];
+          }
+        }
+        lsum[0] = fmaf(add[0], out, lsum[0]);
+        lsum[1] = fmaf(add[1], out, lsum[1]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    });
+    if (more && __builtin_expect(n1.masked, 0)) hide(T, n1, u + 1);
+    const uint4 p[2][2] = {{pb[0][0], pb[0][1]}, {pb[1][0], pb[1][1]}};
+    const float sub1[2] = {ref[0] - n1.lv, ref[1] - n1.lv};
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (K(u + 1) has been read: its stage may be filled; of V only what is used next is waited for early)
+    if (KIND == 1) copy_all(n3, false, kn);
+    bf16x8 vop = v_op(vr[0], 0), vop1;
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 1");  // (two wait states between the operands and the first matrix instruction)
+    in_steps<PH>([&](auto number) {
+      constexpr int j = decltype(number)::value, i = j >> 1;
+      constexpr bool copies = KIND == 2 && j % kEvery == 0 && j / kEvery < NC;
+      if (copies) copy_aim(false, kn, j / kEvery);
+      mm_o<D, F16>(o[i % DVB][j & 1], vop, __builtin_bit_cast(bf16x8, p[j & 1][i / DVB]));
+      __builtin_amdgcn_sched_barrier(0);
+      if (copies) copy_piece(n3, false, j / kEvery);
+      if (more && j == PH - 2 * kAhead) {  // K(u + 2) has landed; newer: V(u + 1) and what has been requested of K(u + 3)
+        constexpr int part = (PH - 2 * kAhead) / kEvery + 1 < NC ? (PH - 2 * kAhead) / kEvery + 1 : NC;
+        win_wait<NC + (KIND == 2 ? part : NC)>();
+      }
+      if constexpr (j % 2 == 0) {
+        constexpr int to = i + kAhead;
+        if constexpr (to < KS) {
+          if constexpr (to < NV) vr[to] = read_v(vc_, to);
+        } else if constexpr (more && !(PAGED && (to - KS) % 2)) {
+          kcur[PAGED ? (to - KS) / 2 : to - KS] = read_k(par, PAGED ? (to - KS) / 2 : to - KS);
+        }
+        if constexpr (i + 1 < KS) {
+          vop1 = v_op(vr[(i + 1) % NV], (i + 1) / DVB);
+          if (PAGED) asm volatile("" : "+v"(vop1));  // (made here, two instructions and more ahead of its use)
+        }
+      } else {
+        vop = vop1;
+      }
+      if (more) p_ops(T, std::integral_constant<int, ticks.ahead[TK::in_pv(j)]>{}, std::integral_constant<int, ticks.ahead[TK::in_pv(j + 1)]>{}, n1.f, sub1);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (D == 128 && KIND < 2) mfma_fence();  // (O may be moved to other registers between one form of this and another)
+    cur = n1;
+    n1 = n2;
+    n2 = n3;
+  };
+  if (nu > 0) {
+    const std::integral_constant<int, 0> even, last;
+    const std::integral_constant<int, 1> odd, edge;
+    const std::integral_constant<int, 2> steady;
+    // units whose copies (of the next one's V and of K three on) are of 32 rows that are there: not the last of either run of keys
+    int whole = nu - 1;
+    if constexpr (!PAGED)
+      whole = kc.plain(nk - 32 * (walk.n_sink - 1)) && vc.plain(32) ? (walk.n - 1 - wave + NW - 1) / NW - 3 : 0;
+    int u = 0;
+    for (; u + 1 < whole; u += 2) {
+      body(steady, even, s0, s1, u);
+      body(steady, odd, s1, s0, u + 1);
+    }
+    if (D == 128) mfma_fence();
+    for (; u + 2 < nu; u += 2) {
+      body(edge, even, s0, s1, u);
+      body(edge, odd, s1, s0, u + 1);
+    }
+    if (u + 1 < nu) {
+      body(edge, even, s0, s1, u);
+      body(last, odd, s1, s0, u + 1);
+    } else {
+      body(last, even, s0, s1, u);
+    }
+    win_wait<0>();  // (the copies made for units behind the last one land before their place is used again)
+  }
+  mfma_fence();  // the last matrix results land before they are read
+#pragma unroll
+  for (int x = 0; x < DVB; ++x) pin_o(o[x][0]), pin_o(o[x][1]);
+  __builtin_amdgcn_sched_barrier(0);
 
   // merge: reference and sum of a column by way of LDS, O normalised by its own wavefront
   float M[2], L[2], fac[2];

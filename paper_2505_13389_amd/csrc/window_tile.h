@@ -79,30 +79,41 @@ __device__ __forceinline__ void win_wait() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Copies of 32 rows with any stride by one wavefront: instruction c fills LDS rows c*RPI .., swizzled on the source side.
+// Copies of 32 rows with any stride by one wavefront: instruction c fills LDS rows c*RPI .., swizzled on the source side.  Four
+// of them share a value of M0 (their immediate offsets are added to both addresses, the lane offsets make up for the global one, which
+// takes rows that are at least as far apart as in LDS) and their lane offsets: the swizzle repeats after 16 rows.
 template <int D>
 struct RowCopy {
   using TL = Tile<D>;
   static constexpr int NC = 32 / TL::RPI;
-  unsigned off[NC];
-  __device__ __forceinline__ unsigned at(int c, int lane, unsigned stride, int last) const {
+  unsigned off[4];
+  unsigned stride;
+  __device__ __forceinline__ unsigned at(int c, int lane, int last) const {
     const int x = c * TL::RPI + lane / TL::CPR, pc = lane % TL::CPR;
     return (unsigned)min(x, last) * stride + ((pc ^ TL::swz(x)) << 4);
   }
-  __device__ __forceinline__ void init(int lane, unsigned stride) {
+  __device__ __forceinline__ void init(int lane, unsigned stride_) {
+    stride = stride_;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) off[c] = at(c, lane, stride, 31);
+    for (int c = 0; c < 4; ++c) off[c] = at(c, lane, 31) - (unsigned)c * 1024u;
   }
-  __device__ __forceinline__ void piece(const void* base, unsigned lds, int c) const { win_copy16(base, off[c], lds + (unsigned)c * 1024u); }
+  // 32 rows are there, far enough apart: piece by piece
+  __device__ __forceinline__ bool plain(int have) const { return have >= 32 && stride >= TL::ROW_BYTES; }
+  __device__ __forceinline__ void aim(unsigned lds, int c) const {
+    if (c % 4 == 0) set_m0_ahead(lds + (unsigned)c * 1024u);
+  }
+  // (aim(lds, c) and another instruction came before it)
+  __device__ __forceinline__ void piece(const unsigned char* base, int c) const {
+    const unsigned char* g = c < 4 ? base : base + 4 * TL::RPI * (long long)stride;
+    if (c % 4 == 0) lds_dma16_at<0>(g, off[c % 4]);
+    if (c % 4 == 1) lds_dma16_at<1024>(g, off[c % 4]);
+    if (c % 4 == 2) lds_dma16_at<2048>(g, off[c % 4]);
+    if (c % 4 == 3) lds_dma16_at<3072>(g, off[c % 4]);
+  }
   // `have` rows are there: the last of them stands for those behind it
-  __device__ __forceinline__ void all(const void* base, unsigned lds, int lane, unsigned stride, int have) const {
-    if (have >= 32) {
+  __device__ __forceinline__ void all(const unsigned char* base, unsigned lds, int lane, int have) const {
 #pragma unroll
-      for (int c = 0; c < NC; ++c) piece(base, lds, c);
-    } else {
-#pragma unroll
-      for (int c = 0; c < NC; ++c) win_copy16(base, at(c, lane, stride, have - 1), lds + (unsigned)c * 1024u);
-    }
+    for (int c = 0; c < NC; ++c) win_copy16(base, at(c, lane, min(have, 32) - 1), lds + (unsigned)c * 1024u);
   }
 };
 
