@@ -64,8 +64,6 @@ int check_window(const vsa_window_t* p) {
 // rows of the query tensors; `packed` by whether offsets are given
 long long stat_rows(const vsa_window_t* p, bool packed) { return packed ? p->total_q : (long long)p->B * p->max_q; }
 
-size_t bwd_bytes(const vsa_window_t* p, long long rows) { return (size_t)p->H * rows * sizeof(float2) + 16; }
-
 WinArgs window_args(const vsa_window_t* p, bool packed, const int32_t* cu_q, const int32_t* cu_k) {
   WinArgs a = {};
   a.mask = {p->unit, p->left, p->right, p->sinks};
@@ -76,6 +74,10 @@ WinArgs window_args(const vsa_window_t* p, bool packed, const int32_t* cu_q, con
   a.scale = scale_or_default(p->softmax_scale, p->d);
   return a;
 }
+
+// of the backward: the rows' terms, then partial results
+size_t terms_bytes(const WinArgs& a) { return ((size_t)a.H * a.lse_rows * 8 + 255) / 256 * 256; }
+size_t bwd_bytes(const vsa_window_t* p, const WinArgs& a) { return terms_bytes(a) + vsa::window_parts(a, p->d) * sizeof(float) + 16; }
 
 int check_window_strides(const vsa_window_t* p, bool packed, bool backward) {
   const long long nb = packed ? 1 : p->B, nq = packed ? p->total_q : p->max_q, nk = packed ? p->total_k : p->max_k;
@@ -209,8 +211,8 @@ int vsa_window_forward(const vsa_window_t* p, const void* q, const void* k, cons
 
 size_t vsa_window_workspace_bytes(const vsa_window_t* p) {
   if (check_window(p) != VSA_OK) return 0;
-  const long long dense = (long long)p->B * p->max_q;
-  return bwd_bytes(p, dense > p->total_q ? dense : p->total_q);
+  const size_t dense = bwd_bytes(p, window_args(p, false, nullptr, nullptr)), packed = bwd_bytes(p, window_args(p, true, nullptr, nullptr));
+  return dense > packed ? dense : packed;
 }
 
 int vsa_window_backward(const vsa_window_t* p, const void* q, const void* k, const void* v, const int32_t* cu_q,
@@ -226,14 +228,15 @@ int vsa_window_backward(const vsa_window_t* p, const void* q, const void* k, con
       off(cu_q, 4) || off(cu_k, 4) || off(workspace, 16))
     return VSA_ERR_ALIGN;
   if ((rc = check_window_strides(p, packed, true)) != VSA_OK) return rc;
-  if (!workspace || workspace_bytes < bwd_bytes(p, rows)) return VSA_ERR_WORKSPACE;
   WinArgs a = window_args(p, packed, cu_q, cu_k);
+  if (!workspace || workspace_bytes < bwd_bytes(p, a)) return VSA_ERR_WORKSPACE;
   a.q = view(q, p->q, packed), a.k = view(k, p->k, packed), a.v = view(v, p->v, packed), a.o = view(out, p->out, packed);
   a.dout = view(dout, p->dout, packed), a.dq = view(dq, p->dq, packed), a.dk = view(dk, p->dk, packed), a.dv = view(dv, p->dv, packed);
   a.lse = const_cast<float*>(lse);
-  a.stats = (float2*)workspace;
+  a.stats = (float*)workspace;
+  float* const parts = (float*)((unsigned char*)workspace + terms_bytes(a));
   hipStream_t s = (hipStream_t)hip_stream;
-  VSA_LAUNCH("window_bwd", vsa::launch_window_bwd(a, p->d, p->dtype == VSA_DTYPE_FP16, s));
+  VSA_LAUNCH("window_bwd", vsa::launch_window_bwd(a, p->d, p->dtype == VSA_DTYPE_FP16, parts, s));
   return VSA_OK;
 }
 

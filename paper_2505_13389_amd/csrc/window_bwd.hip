@@ -6,12 +6,15 @@
 // The second sums shared heads on the way, in order: no atomics, the same bits every time.  S and dP are formed twice (7 products
 // for 5), which costs less than passing P and dS through memory.  As in the forward a lane owns columns of 32 (queries, keys), the
 // other index runs through its registers, and what has been formed in them is the operand of the product over that index.
+#include <type_traits>
+
+#include "unit_stream.h"
 #include "window_kernels.h"
 #include "window_tile.h"
 
 namespace vsa {
 
-// D and the log-sum-exp in log2 units, a float2 a row: 8 elements a lane
+// -lse / scale (-inf for a row that sees nothing) and -D, a plane each: what S and dP start from.  8 elements a lane.
 template <int D, bool F16>
 __global__ __launch_bounds__(256) void k_window_stats(WinArgs a) {
   constexpr int CPR = D / 8;
@@ -31,22 +34,77 @@ __global__ __launch_bounds__(256) void k_window_stats(WinArgs a) {
   for (int m = CPR / 2; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
   if (at >= n || ch) return;
   const float lse = a.lse[h * a.lse_rows + row];
-  a.stats[h * a.lse_rows + row] = make_float2(lse == -INFINITY ? INFINITY : lse * kLog2e, sum);
+  a.stats[h * a.lse_rows + row] = lse == -INFINITY ? -INFINITY : -lse / a.scale;
+  a.stats[n + h * a.lse_rows + row] = -sum;
+}
+
+// Accumulators in the accumulation registers (256 + 256 registers a wavefront at d = 128, see mfma_a).
+template <int D, bool F16>
+__device__ __forceinline__ void mm_acc(f32x16& acc, bf16x8 a, bf16x8 b) {
+  if constexpr (D == 64) acc = mm32<F16>(a, b, acc);
+  else if constexpr (F16) asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+  else mfma_a(acc, a, b);
+}
+template <int D>
+__device__ __forceinline__ void pin_acc(f32x16& acc) {
+  if (D == 128) asm volatile("" : "+a"(acc));
+  else asm volatile("" : "+v"(acc));
+}
+// accumulators in ordinary registers, from the values of c (INIT), or on
+template <int D, bool F16, bool INIT>
+__device__ __forceinline__ void mm_v(f32x16& d, bf16x8 a, bf16x8 b, const f32x16& c) {
+  if constexpr (D == 64) d = mm32<F16>(a, b, INIT ? c : d);
+  else if constexpr (F16) {
+    if constexpr (INIT) asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %3" : "=&v"(d) : "v"(a), "v"(b), "v"(c));
+    else asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
+  } else {
+    if constexpr (INIT) mfma_v_from(d, a, b, c);
+    else mfma_v(d, a, b);
+  }
+}
+template <int D, bool F16>
+__device__ __forceinline__ void mm_v_zero(f32x16& d, bf16x8 a, bf16x8 b) {
+  if constexpr (D == 64) {
+    f32x16 zero;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+    d = mm32<F16>(a, b, zero);
+  } else if constexpr (F16) asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "v"(b));
+  else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "v"(b));
+}
+// products whose second operand (Q, which is read by these alone) is in the accumulation registers at d = 128; FIRST: from zero
+template <int D, bool F16, bool FIRST>
+__device__ __forceinline__ void mm_q(f32x16& d, bf16x8 a, bf16x8 q) {
+  if constexpr (D == 64) {
+    f32x16 zero;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+    d = mm32<F16>(a, q, FIRST ? zero : d);
+  } else if constexpr (F16) {
+    if constexpr (FIRST) asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "a"(q));
+    else asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "a"(q));
+  } else {
+    if constexpr (FIRST) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "a"(q));
+    else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "a"(q));
+  }
 }
 
 // accumulator tiles [32 x ..][64 columns] of NW wavefronts -> rows of 16 bits, scaled; `buf`: 64 * D floats a wavefront
 template <int D, bool F16, int NW, int CT, class ROW>
-__device__ __forceinline__ void store_columns(const f32x16 (&acc)[D / 32][CT], float scale, float* buf, int tid, int rows, const ROW& row_of) {
+__device__ __forceinline__ void store_columns(f32x16 (&acc)[D / 32][CT], float scale, float* buf, int pitch, int tid, int rows, const ROW& row_of) {
   const int lane = tid & 63, wave = tid >> 6, l32 = lane & 31, h = lane >> 5;
-  float* const mine = buf + wave * 32 * CT * D;
+  float* const mine = buf + wave * pitch;
 #pragma unroll
   for (int t = 0; t < CT; ++t)
 #pragma unroll
-    for (int x = 0; x < D / 32; ++x)
+    for (int x = 0; x < D / 32; ++x) {
+      pin_acc<D>(acc[x][t]);  // (a tile at a time in ordinary registers)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         *(float4*)&mine[merge_offset(t * 32 + l32, x * 32 + 8 * i + 4 * h, D)] =
             make_float4(acc[x][t][4 * i], acc[x][t][4 * i + 1], acc[x][t][4 * i + 2], acc[x][t][4 * i + 3]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   if (NW > 1) __syncthreads();
   else __builtin_amdgcn_wave_barrier();
   for (int it = tid; it < rows * (D / 8); it += 64 * NW) {
@@ -54,7 +112,7 @@ __device__ __forceinline__ void store_columns(const f32x16 (&acc)[D / 32][CT], f
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float* q = buf + w * 32 * CT * D;
+      const float* q = buf + w * pitch;
       const float4 x = *(const float4*)&q[merge_offset(r, ch * 8, D)], y = *(const float4*)&q[merge_offset(r, ch * 8 + 4, D)];
       v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
     }
@@ -65,11 +123,48 @@ __device__ __forceinline__ void store_columns(const f32x16 (&acc)[D / 32][CT], f
   }
 }
 
+// the same into a slot of partial results, [64][D] floats
+template <int D, int NW>
+__device__ __forceinline__ void store_part(f32x16 (&acc)[D / 32][2], float* buf, int tid, int rows, float* slot) {
+  const int lane = tid & 63, wave = tid >> 6, l32 = lane & 31, h = lane >> 5;
+  float* const mine = buf + wave * 64 * D;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x) {
+      pin_acc<D>(acc[x][t]);  // (a tile at a time in ordinary registers)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(float4*)&mine[merge_offset(t * 32 + l32, x * 32 + 8 * i + 4 * h, D)] =
+            make_float4(acc[x][t][4 * i], acc[x][t][4 * i + 1], acc[x][t][4 * i + 2], acc[x][t][4 * i + 3]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  if (NW > 1) __syncthreads();
+  else __builtin_amdgcn_wave_barrier();
+  for (int it = tid; it < rows * (D / 4); it += 64 * NW) {
+    const int r = it / (D / 4), ch = it % (D / 4);
+    float4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float4 x = *(const float4*)&buf[w * 64 * D + merge_offset(r, ch * 4, D)];
+      v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+    }
+    *(float4*)&slot[r * D + ch * 4] = v;
+  }
+}
+
+// dQ.  The products of a unit, in this order, and what lies behind their matrix instructions:
+//   dP(u) = V dO^T     the rest of P(u), copies of K(u + 2)
+//   S(u + 1) = K Q^T   dS(u)
+//   dQ += K^T dS(u)    the first of P(u + 1), copies of V(u + 2)
+// K has three stages (of unit u to its end, of u + 1, of u + 2), V two.
 template <int D, bool F16, int NW>
 __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, unsigned items, int nqb, int chunked) {
   using TL = Tile<D>;
-  constexpr int KS = D / 16, DVB = D / 32, HALF = 32 * D * 2, NC = RowCopy<D>::NC;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * 4 * HALF];
+  constexpr int KS = D / 16, DVB = D / 32, HALF = 32 * D * 2, NC = RowCopy<D>::NC, PH = 2 * KS, IPM = 16 / PH;  // softmax items a matrix instruction
+  constexpr int kAhead = 2, kEvery = PH / NC, kEarly = 4;  // kEarly: items of P done in the phase before its own
+  constexpr int STAGES = 5 * HALF, PLACE = STAGES > 64 * D * 4 ? STAGES : 64 * D * 4;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * PLACE];
   int b;
   unsigned item;
   if (!win_item(blockIdx.x, items, chunked != 0, b, item)) return;
@@ -84,16 +179,17 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, unsigned it
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, h = lane >> 5;
   const int nu = walk.n > wave ? (walk.n - wave + NW - 1) / NW : 0;
+  const float sl2 = a.scale * kLog2e;
 
   WinSpan span[2];
-  float lse2[2], delta[2];
+  float from[2], minus[2];  // exponents start from, -D
   bf16x8 qreg[2][KS], dreg[2][KS];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const int r = min(r0 + 32 * t + l32, sq.n - 1);
     span[t] = win_span(a.mask, r + shift, nk);
-    const float2 st = a.stats[a.stat(hq, b, sq.row0, r)];
-    lse2[t] = st.x, delta[t] = st.y;
+    const long long st = a.stat(hq, b, sq.row0, r);
+    from[t] = a.stats[st] * sl2, minus[t] = a.stats[a.lse_rows * a.H + st];
     const uint4 *p = (const uint4*)a.q.row(b, sq.row0 + r, hq), *pd = (const uint4*)a.dout.row(b, sq.row0 + r, hq);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -102,254 +198,689 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, unsigned it
     }
   }
 #pragma unroll
-  for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qreg[0][s]), "+v"(qreg[1][s]), "+v"(dreg[0][s]), "+v"(dreg[1][s]));
-  asm volatile("" : "+v"(lse2[0]), "+v"(lse2[1]), "+v"(delta[0]), "+v"(delta[1]));
+  for (int s = 0; s < KS; ++s)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (D == 128) asm volatile("" : "+a"(qreg[t][s]));
+      else asm volatile("" : "+v"(qreg[t][s]));
+      asm volatile("" : "+v"(dreg[t][s]));
+    }
+  asm volatile("" : "+v"(from[0]), "+v"(from[1]), "+v"(minus[0]), "+v"(minus[1]));
 
-  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem)) + (unsigned)wave * (4 * HALF);
-  unsigned char* const mine = smem + wave * (4 * HALF);
-  const unsigned kstride = (unsigned)a.k.token, vstride = (unsigned)a.v.token;
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem)) + (unsigned)wave * PLACE;
+  unsigned char* const mine = smem + wave * PLACE;
   const unsigned char* kb = (const unsigned char*)uniform_ptr(a.k.row(b, sk.row0, hk));
   const unsigned char* vb = (const unsigned char*)uniform_ptr(a.v.row(b, sk.row0, hk));
   RowCopy<D> kc, vc;
-  kc.init(lane, kstride);
-  vc.init(lane, vstride);
-  auto copy = [&](int u, int stage) {
-    const int at = walk.begin(wave + NW * u);
-    kc.all(kb + (long long)at * kstride, lds0 + stage * HALF, lane, nk - at);
-    vc.all(vb + (long long)at * vstride, lds0 + (2 + stage) * HALF, lane, nk - at);
+  kc.init(lane, (unsigned)a.k.token);
+  vc.init(lane, (unsigned)a.v.token);
+  auto first_key = [&](int u) { return walk.begin(wave + NW * min(u, nu - 1)); };  // (units behind the last: that one again)
+  auto copy_all = [&](const RowCopy<D>& c, const unsigned char* base, int key, unsigned lds) {
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    c.all(base + (long long)key * c.stride, lds, l, nk - key);
   };
-  f32x16 acc[DVB][2], zero16;
+  constexpr int kV = 3 * HALF;  // of the V stages
+
+  f32x16 acc[DVB][2];
+  float nil = 0.f;
+  asm volatile("" : "+v"(nil));
 #pragma unroll
-  for (int i = 0; i < 16; ++i) zero16[i] = 0.f;
+  for (int x = 0; x < DVB; ++x)
 #pragma unroll
-  for (int x = 0; x < DVB; ++x) acc[x][0] = acc[x][1] = zero16;
-  const float sl2 = a.scale * kLog2e;
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[x][t][i] = nil;
+      pin_acc<D>(acc[x][t]);
+    }
   const int lane_a = TL::rowmajor_lane(0, lane);
   int b0, b1;
   TL::transposed_lane(0, lane, b0, b1);
-
-  if (nu > 0) copy(0, 0);
-  for (int u = 0; u < nu; ++u) {
-    const int par = u & 1, piece = wave + NW * u;
-    if (u + 1 < nu) {
-      copy(u + 1, 1 - par);
-      win_wait<2 * NC>();
-    } else {
-      win_wait<0>();
-    }
-    const unsigned char *ks = mine + par * HALF, *vs = mine + (2 + par) * HALF;
-    f32x16 s[2], p[2];
+  auto hide = [&](f32x16 (&S)[2], int u) {
+    int first = 4 * h;
+    asm volatile("" : "+v"(first));
+    first += first_key(u);
 #pragma unroll
-    for (int st = 0; st < KS; ++st) {
-      const bf16x8 ka = TL::rowmajor_at(ks, lane_a, st), va = TL::rowmajor_at(vs, lane_a, st);
+    for (int t = 0; t < 2; ++t) {
+      const WinSpan w = walk.span_in(wave + NW * u, span[t]);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        s[t] = mm32<F16>(ka, qreg[t][st], st == 0 ? zero16 : s[t]);
-        p[t] = mm32<F16>(va, dreg[t][st], st == 0 ? zero16 : p[t]);
+      for (int i = 0; i < 16; ++i) {
+        const int key = first + 8 * (i >> 2) + (i & 3);
+        S[t][i] = key < w.hi && (key >= w.lo || key < w.se) ? S[t][i] : -INFINITY;
       }
     }
-    const int key0 = walk.begin(piece);
+  };
+  // P of item `it` in place of S: exponents, then exponentials
+  auto p_arg = [&](f32x16 (&S)[2], int it) {
+    const int t = (it >> 2) & 1, e = 8 * (it >> 3) + 2 * (it & 3);
+    for (int i = 0; i < 2; ++i) {
+      S[t][e + i] = fmaf(S[t][e + i], sl2, from[t]);
+      asm volatile("" : : "v"(S[t][e + i]));
+    }
+  };
+  auto p_exp = [&](f32x16 (&S)[2], int it) {
+    const int t = (it >> 2) & 1, e = 8 * (it >> 3) + 2 * (it & 3);
+    for (int i = 0; i < 2; ++i) {
+      S[t][e + i] = fast_exp2(S[t][e + i]);
+      asm volatile("" : : "v"(S[t][e + i]));
+    }
+  };
+  // slot n of 17: the argument of item n, the exponential of the one before
+  auto p_slots = [&](f32x16 (&S)[2], int from_slot, int to_slot) {
+#pragma unroll
+    for (int n = from_slot; n < to_slot; ++n) {
+      if (n < 16) p_arg(S, n);
+      if (n > 0) p_exp(S, n - 1);
+    }
+  };
+  uint32_t dsw[2][2][4];
+  auto d_sub = [&](f32x16 (&dp)[2], int it) {
+    const int t = (it >> 2) & 1, e = 8 * (it >> 3) + 2 * (it & 3);
+    for (int i = 0; i < 2; ++i) {
+      dp[t][e + i] += minus[t];
+      asm volatile("" : : "v"(dp[t][e + i]));
+    }
+  };
+  auto d_mul = [&](f32x16 (&dp)[2], const f32x16 (&S)[2], int it) {
+    const int t = (it >> 2) & 1, e = 8 * (it >> 3) + 2 * (it & 3);
+    for (int i = 0; i < 2; ++i) {
+      dp[t][e + i] *= S[t][e + i];
+      asm volatile("" : : "v"(dp[t][e + i]));
+    }
+  };
+  auto d_cvt = [&](const f32x16 (&dp)[2], int it) {
+    const int t = (it >> 2) & 1, e = 8 * (it >> 3) + 2 * (it & 3);
+    dsw[t][it >> 3][it & 3] = pack16<F16>(dp[t][e], dp[t][e + 1]);
+    asm volatile("" : : "v"(dsw[t][it >> 3][it & 3]));
+  };
+  auto d_slots = [&](f32x16 (&dp)[2], const f32x16 (&S)[2], int from_slot, int to_slot) {
+#pragma unroll
+    for (int n = from_slot; n < to_slot; ++n) {
+      if (n < 16) d_sub(dp, n);
+      if (n > 0 && n < 17) d_mul(dp, S, n - 1);
+      if (n > 1 && n < 18) d_cvt(dp, n - 2);
+    }
+  };
+  f32x16 s0[2], s1[2];
+  unsigned k_at = 0;  // stage of K(u), bytes
+  auto after = [](unsigned x) { return x == 2u * HALF ? 0u : x + HALF; };
+  auto rows_of = [&](unsigned stage, int s) { return TL::rowmajor_at(mine + stage, lane_a, s); };
+  bf16x8 vcur[kAhead];
+  if (nu > 0) {
+    copy_all(kc, kb, first_key(0), lds0);
+    copy_all(vc, vb, first_key(0), lds0 + kV);
+    copy_all(kc, kb, first_key(1), lds0 + HALF);
+    copy_all(vc, vb, first_key(1), lds0 + kV + HALF);
+    win_wait<2 * NC>();
+    in_steps<KS>([&](auto number) {
+      constexpr int s = decltype(number)::value;
+      const bf16x8 ka = rows_of(0, s);
+      mm_q<D, F16, s == 0>(s0[0], ka, qreg[0][s]);
+      mm_q<D, F16, s == 0>(s0[1], ka, qreg[1][s]);
+    });
+    mfma_fence();
+    if (walk.masked(wave)) hide(s0, 0);
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) vcur[s] = rows_of(kV, s);
+    p_slots(s0, 0, kEarly);
+  }
+  // STEADY: the copies are of 32 rows that are there, piece by piece; else at once, and u may be the last unit.  `par` = u & 1 (a
+  // constant in the unrolled loop).
+  auto body = [&](auto steady_tag, int par, f32x16 (&S)[2], f32x16 (&T)[2], int u) {
+    constexpr bool STEADY = decltype(steady_tag)::value;
+    const bool more = STEADY || u + 1 < nu;
+    const unsigned k1 = after(k_at), k2 = after(k1);
+    const int key2 = first_key(u + 2);
+    const unsigned char *kp = kb + (long long)key2 * kc.stride, *vp = vb + (long long)key2 * vc.stride;
+    f32x16 dp[2];
+    bf16x8 vr[KS], kr[KS], tr[KS];
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) vr[s] = vcur[s];
+    if (!STEADY) copy_all(kc, kb, key2, lds0 + k2);
+    __builtin_amdgcn_sched_barrier(0);
+    in_steps<PH>([&](auto number) {  // dP(u)
+      constexpr int j = decltype(number)::value, s = j >> 1;
+      constexpr bool copies = STEADY && j % kEvery == 0;
+      if (copies) {
+        kc.aim(lds0 + k2, j / kEvery);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (s == 0) mm_v_zero<D, F16>(dp[j & 1], vr[s], dreg[j & 1][s]);
+      else mm_v<D, F16, false>(dp[j & 1], vr[s], dreg[j & 1][s], dp[j & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (copies) kc.piece(kp, j / kEvery);
+      if (j == PH - 2 * kAhead) {  // K(u + 1) has landed; newer: V(u + 1) and what has been requested of K(u + 2)
+        constexpr int part = STEADY ? j / kEvery + 1 : NC;
+        win_wait<NC + part>();
+      }
+      if (j % 2 == 0) {
+        constexpr int to = s + kAhead;
+        if constexpr (to < KS) vr[to] = rows_of(kV + par * HALF, to);
+        else kr[to - KS] = rows_of(k1, to - KS);
+      }
+      constexpr int n0 = kEarly + (17 - kEarly) * j / PH, n1 = kEarly + (17 - kEarly) * (j + 1) / PH;
+      p_slots(S, n0, n1);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    auto t_op = [&](int i) { return TL::transposed_at(mine + k_at, b0, b1, i / DVB, i % DVB); };
+    constexpr int kLag = 2;  // dP is complete that many matrix instructions on
+    in_steps<PH>([&](auto number) {  // S(u + 1)
+      constexpr int j = decltype(number)::value, s = j >> 1;
+      mm_q<D, F16, s == 0>(T[j & 1], kr[s], qreg[j & 1][s]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (j % 2 == 0) {
+        constexpr int to = s + kAhead;
+        if constexpr (to < KS) {
+          kr[to] = rows_of(k1, to);
+        } else {
+          tr[to - KS] = t_op(to - KS);
+        }
+      }
+      constexpr int n0 = j < kLag ? 0 : 18 * (j - kLag) / (PH - kLag), n1 = j < kLag ? 0 : 18 * (j + 1 - kLag) / (PH - kLag);
+      d_slots(dp, S, n0, n1);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (more && __builtin_expect(walk.masked(wave + NW * min(u + 1, nu - 1)), 0)) {
+      if (D == 128) mfma_fence();
+      hide(T, u + 1);
+    }
+    if (!STEADY) copy_all(vc, vb, key2, lds0 + kV + par * HALF);
+    bf16x8 ds[2][2];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[t][i] = fast_exp2(fmaf(s[t][i], sl2, -lse2[t])) * (p[t][i] - delta[t]);
-    if (walk.masked(piece)) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const WinSpan w = walk.span_in(piece, span[t]);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = key0 + 8 * (i >> 2) + 4 * h + (i & 3);
-          s[t][i] = key < w.hi && (key >= w.lo || key < w.se) ? s[t][i] : 0.f;
-        }
-      }
-    }
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      bf16x8 ds[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        uint4 w = {pack16<F16>(s[t][8 * st], s[t][8 * st + 1]), pack16<F16>(s[t][8 * st + 2], s[t][8 * st + 3]),
-                   pack16<F16>(s[t][8 * st + 4], s[t][8 * st + 5]), pack16<F16>(s[t][8 * st + 6], s[t][8 * st + 7])};
-        ds[t] = __builtin_bit_cast(bf16x8, w);
-      }
-#pragma unroll
-      for (int x = 0; x < DVB; ++x) {
-        const bf16x8 ka = TL::transposed_at(ks, b0, b1, st, x);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) acc[x][t] = mm32<F16>(ka, ds[t], acc[x][t]);
-      }
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      for (int st = 0; st < 2; ++st) ds[t][st] = __builtin_bit_cast(bf16x8, make_uint4(dsw[t][st][0], dsw[t][st][1], dsw[t][st][2], dsw[t][st][3]));
     __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 1");
+    in_steps<PH>([&](auto number) {  // dQ
+      constexpr int j = decltype(number)::value, i = j >> 1;
+      constexpr bool copies = STEADY && j % kEvery == 0;
+      if (copies) {
+        vc.aim(lds0 + kV + par * HALF, j / kEvery);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      mm_acc<D, F16>(acc[i % DVB][j & 1], tr[i], ds[j & 1][i / DVB]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (copies) vc.piece(vp, j / kEvery);
+      if (j == PH - 2 * kAhead) {  // V(u + 1) has landed; newer: K(u + 2) and what has been requested of V(u + 2)
+        constexpr int part = STEADY ? j / kEvery + 1 : NC;
+        win_wait<NC + part>();
+      }
+      if (j % 2 == 0) {
+        constexpr int to = i + kAhead;
+        if constexpr (to < KS) tr[to] = t_op(to);
+        else vcur[to - KS] = rows_of(kV + (1 - par) * HALF, to - KS);
+      }
+      // (S(u + 1) is complete and may be read from here on: its last product lies kLag matrix instructions back)
+      constexpr int n0 = j < kLag ? 0 : kEarly * (j - kLag) / (PH - kLag), n1 = j < kLag ? 0 : kEarly * (j + 1 - kLag) / (PH - kLag);
+      p_slots(T, n0, n1);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (D == 128 && !STEADY) mfma_fence();  // (accumulators may be moved between one form of this and another)
+    k_at = k1;
+  };
+  if (nu > 0) {
+    // units whose copies (two on) are of 32 rows that are there: not the last of either run of keys
+    const int whole = kc.plain(nk - 32 * (walk.n_sink - 1)) && vc.plain(32) ? (walk.n - 1 - wave + NW - 1) / NW - 2 : 0;
+    int u = 0;
+    for (; u + 1 < whole; u += 2) {
+      body(std::true_type{}, 0, s0, s1, u);
+      body(std::true_type{}, 1, s1, s0, u + 1);
+    }
+    if (D == 128) mfma_fence();
+    for (; u < nu; ++u) {  // (behind the last unit: that one again)
+      body(std::false_type{}, u & 1, s0, s1, u);
+      s0[0] = s1[0];
+      s0[1] = s1[1];
+    }
+    win_wait<0>();
   }
+  mfma_fence();
+#pragma unroll
+  for (int x = 0; x < DVB; ++x) pin_acc<D>(acc[x][0]), pin_acc<D>(acc[x][1]);
+  __builtin_amdgcn_sched_barrier(0);
   if (NW > 1) __syncthreads();
-  store_columns<D, F16, NW, 2>(acc, a.scale, (float*)smem, tid, rows, [&](int r) { return a.dq.out(b, sq.row0 + r0 + r, hq); });
+  store_columns<D, F16, NW, 2>(acc, a.scale, (float*)smem, PLACE / 4, tid, rows, [&](int r) { return a.dq.out(b, sq.row0 + r0 + r, hq); });
 }
 
-// columns of 32 keys of a wavefront: at d = 128 two need more than 512 registers
-template <int D>
-constexpr int dkv_tiles() { return D == 128 ? 1 : 2; }
+// How the key blocks of a head are cut into workgroups: a block whose queries (of all heads of the group) are more than `per` units is
+// walked in parts of its own, which leave their sums in fp32 to be added, in order, by k_window_join.  Blocks of sinks, which every
+// later query sees, are the long ones.
+struct DkvPlan {
+  int nkb, sink_blocks, sink_parts, parts;  // 64-key blocks of a head, those that may hold sinks, parts of each, of the others
+  int per;
+  long long slots;  // partial results of a head
+  __host__ __device__ int items() const { return sink_blocks * sink_parts + (nkb - sink_blocks) * parts; }
+  // item of a head -> its block, part and how many there may be
+  __host__ __device__ void at(int item, int& block, int& part, int& of) const {
+    const int first = sink_blocks * sink_parts;
+    of = item < first ? sink_parts : parts;
+    block = item < first ? item / of : sink_blocks + (item - first) / of;
+    part = item < first ? item % of : (item - first) % of;
+  }
+  __host__ __device__ int slot(int block, int part) const {
+    return block < sink_blocks ? block * sink_parts + part : sink_blocks * sink_parts + (block - sink_blocks) * parts + part;
+  }
+  // parts that a block of so many units has work for
+  __host__ __device__ int live(int units, int of) const {
+    const int want = (units + per - 1) / per;
+    return want < 1 ? 1 : want < of ? want : of;
+  }
+};
 
+static DkvPlan dkv_plan(const WinArgs& a) {
+  DkvPlan p = {};
+  p.nkb = (a.rk.most + 63) / 64;
+  const WinMask& m = a.mask;
+  const long long most = (a.rq.most + 31) / 32 + 1, blocks = (long long)a.B * a.Hkv;
+  const long long ur_ = m.left < 0 || m.right < 0 ? most : ((long long)(m.left + m.right + 2) * m.unit + 64) / 32 + 2;
+  const long long ur = (ur_ < most ? ur_ : most) * a.G, us = most * a.G;
+  const long long sinks = ur_ < most ? (long long)m.sinks * m.unit : 0, sb = (sinks + 63) / 64;
+  p.sink_blocks = (int)(sb < p.nkb ? sb : p.nkb);
+  const long long total = blocks * (p.sink_blocks * us + (p.nkb - p.sink_blocks) * ur);
+  long long per = total / 1024;  // (512 workgroups at a time: a part is half of what one gets in all, at most)
+  if (per < 32) per = 32;
+  if (per > 1 << 30) per = 1 << 30;
+  p.per = (int)per;
+  auto parts = [&](long long units) { return (int)((units + per - 1) / per < 64 ? (units + per - 1) / per : 64); };
+  p.sink_parts = p.sink_blocks ? parts(us) : 1;
+  p.parts = blocks * p.nkb >= 512 ? 1 : parts(ur);
+  if (p.sink_parts < 1) p.sink_parts = 1;
+  if (p.parts < 1) p.parts = 1;
+  p.slots = p.parts > 1 ? p.items() : p.sink_parts > 1 ? p.sink_blocks * p.sink_parts : 0;
+  return p;
+}
+
+size_t window_parts(const WinArgs& a, int d) { return (size_t)a.B * a.Hkv * dkv_plan(a).slots * (2 * 64 * d); }
+
+// dK, dV.  The products of a unit, in this order, and what lies behind their matrix instructions:
+//   S = Q K^T, from -lse / scale    copies of Q and the row terms of u + 1
+//   dP = dO V^T, from -D            most of P
+//   dV += dO^T P                    the rest of P, most of dS
+//   dK += Q^T dS                    the rest of dS, copies of dO(u + 2)
+// dK and dV are accumulation registers, K and V of the first 32 keys ordinary ones, V of the others is in LDS.
 template <int D, bool F16, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, unsigned items, int nkb, int chunked) {
+__global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan plan, float* __restrict__ parts, unsigned items, int chunked) {
   using TL = Tile<D>;
-  constexpr int KT = dkv_tiles<D>(), KS = D / 16, DVB = D / 32, HALF = 32 * D * 2, NC = RowCopy<D>::NC;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * 4 * HALF];
-  __shared__ __attribute__((aligned(256))) float2 stat_stage[NW][2][32];
+  constexpr int KS = D / 16, DVB = D / 32, HALF = 32 * D * 2, NC = RowCopy<D>::NC, PH = 2 * KS;
+  constexpr int kAhead = 2, kEvery = PH / NC;
+  constexpr int PLACE = 4 * HALF;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * PLACE];
+  __shared__ __attribute__((aligned(1024))) unsigned char vsecond[HALF];
+  __shared__ __attribute__((aligned(256))) float terms[NW][2][64];  // of a unit's 32 rows: what S starts from, dP
+  __shared__ int2 seen_by[NW][64];  // queries that see a key (registers are short)
+  static_assert(PLACE == 64 * D * 4, "the partial results fit the stages");
   int b;
   unsigned item;
   if (!win_item(blockIdx.x, items, chunked != 0, b, item)) return;
-  const int hk = (int)(item / (unsigned)nkb), kblk = (int)(item % (unsigned)nkb);
+  const int per_head = plan.items(), hk = (int)(item / (unsigned)per_head);
+  int kblk, part, of;
+  plan.at((int)(item % (unsigned)per_head), kblk, part, of);
   const WinSeq sq = win_seq(a.rq, b), sk = win_seq(a.rk, b);
-  const int k0 = kblk * (32 * KT), keys = min(32 * KT, sk.n - k0);
+  const int k0 = kblk * 64, keys = min(64, sk.n - k0);
   if (keys <= 0) return;
-  const int shift = sk.n - sq.n;
-  const KeyWalk walk(a.mask, k0, k0 + keys, sq.n, shift, 32);
+  const int nq = __builtin_amdgcn_readfirstlane(sq.n), shift = sk.n - nq;
+  const KeyWalk walk(a.mask, k0, k0 + keys, nq, shift, 32);
+  const int wn = __builtin_amdgcn_readfirstlane(walk.n), wfrom = __builtin_amdgcn_readfirstlane(walk.from);
+  auto clamp_q = [&](long long x) { return __builtin_amdgcn_readfirstlane((int)(x < 0 ? 0 : x > nq ? nq : x)); };
+  const int seen_from = clamp_q(walk.seen_from - shift), seen_to = clamp_q(walk.seen_to - shift);
+  const int all = wn * a.G, live = plan.live(all, of);
+  if (part >= live) return;
+  const int begin = (int)((long long)all * part / live), end = (int)((long long)all * (part + 1) / live);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, h = lane >> 5;
-  const int all = walk.n * a.G, nu = all > wave ? (all - wave + NW - 1) / NW : 0;
+  const int nu = end - begin > wave ? (end - begin - wave + NW - 1) / NW : 0;
 
-  int from[KT], to[KT];  // queries that see the lane's keys
-  bf16x8 kreg[KT][KS], vreg[KT][KS];
+  bf16x8 kreg[2][KS], vreg[KS];
 #pragma unroll
-  for (int t = 0; t < KT; ++t) {
+  for (int t = 0; t < 2; ++t) {
     const int j = min(k0 + 32 * t + l32, sk.n - 1);
     const KeySpan w = key_span(a.mask, j);
-    auto clamp = [&](long long x) { return (int)(x < 0 ? 0 : x > sq.n ? sq.n : x); };
-    from[t] = clamp(w.lo - shift);
-    to[t] = clamp(w.hi - shift);
+    auto clamp = [&](long long x) { return (int)(x < 0 ? 0 : x > nq ? nq : x); };
+    if (h == 0) seen_by[wave][32 * t + l32] = make_int2(clamp(w.lo - shift), clamp(w.hi - shift));
     const uint4 *p = (const uint4*)a.k.row(b, sk.row0 + j, hk), *pv = (const uint4*)a.v.row(b, sk.row0 + j, hk);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       kreg[t][s] = __builtin_bit_cast(bf16x8, p[2 * s + h]);
-      vreg[t][s] = __builtin_bit_cast(bf16x8, pv[2 * s + h]);
+      if (t == 0) vreg[s] = __builtin_bit_cast(bf16x8, pv[2 * s + h]);
+      else if (wave == 0) *(uint4*)(vsecond + TL::off(l32, 2 * s + h)) = pv[2 * s + h];
     }
   }
 #pragma unroll
-  for (int t = 0; t < KT; ++t)
-#pragma unroll
-    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(kreg[t][s]), "+v"(vreg[t][s]));
+  for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(kreg[0][s]), "+v"(kreg[1][s]), "+v"(vreg[s]));
+  if (NW > 1) __syncthreads();
+  else __builtin_amdgcn_wave_barrier();
 
-  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem)) + (unsigned)wave * (4 * HALF);
-  const unsigned stat0 = __builtin_amdgcn_readfirstlane(lds_address(stat_stage)) + (unsigned)wave * 512u;
-  unsigned char* const mine = smem + wave * (4 * HALF);
-  const unsigned qstride = (unsigned)a.q.token, dstride = (unsigned)a.dout.token;
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem)) + (unsigned)wave * PLACE;
+  const unsigned terms0 = __builtin_amdgcn_readfirstlane(lds_address(terms)) + (unsigned)wave * 512u;
+  unsigned char* const mine = smem + wave * PLACE;
   RowCopy<D> qc, dc;
-  qc.init(lane, qstride);
-  dc.init(lane, dstride);
-  auto copy = [&](int u, int stage) {
-    const int i = wave + NW * u, g = i / walk.n, at = walk.from + (i - g * walk.n) * 32, hq = hk * a.G + g, have = sq.n - at;
-    const unsigned char* qb = (const unsigned char*)uniform_ptr(a.q.row(b, sq.row0 + at, hq));
-    const unsigned char* db = (const unsigned char*)uniform_ptr(a.dout.row(b, sq.row0 + at, hq));
-    const void* sb = uniform_ptr(a.stats + a.stat(hq, b, sq.row0, at));
-    qc.all(qb, lds0 + stage * HALF, lane, have);
-    dc.all(db, lds0 + (2 + stage) * HALF, lane, have);
-    lds_dma4<4>(sb, (unsigned)min(lane >> 1, have - 1) * 8u + (lane & 1) * 4u, stat0 + stage * 256u);
+  qc.init(lane, (unsigned)a.q.token);
+  dc.init(lane, (unsigned)a.dout.token);
+  const unsigned plane = (unsigned)(a.lse_rows * a.H) * 4u;
+  const unsigned term_off = (unsigned)(lane & 31) * 4u + (lane < 32 ? 0u : plane);
+  // where a unit lies: head of the group and first query
+  struct U {
+    int q;
+    const unsigned char *qp, *dp, *st;
   };
-  f32x16 dk[DVB][KT], dv[DVB][KT], zero16;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) zero16[i] = 0.f;
+  const unsigned char* const q_base = (const unsigned char*)uniform_ptr(a.q.row(b, sq.row0, hk * a.G));
+  const unsigned char* const d_base = (const unsigned char*)uniform_ptr(a.dout.row(b, sq.row0, hk * a.G));
+  const unsigned char* const s_base = (const unsigned char*)uniform_ptr(a.stats + a.stat(hk * a.G, b, sq.row0, 0));
+  // units follow one another: first query and head advance with them
+  int at_g = 0, at_i = 0;
+  auto unit_at = [&](int i) {  // of the walk over all heads
+    at_g = i / wn;
+    at_i = i - at_g * wn;
+    at_g = __builtin_amdgcn_readfirstlane(at_g);
+    at_i = __builtin_amdgcn_readfirstlane(at_i);
+  };
+  auto unit_here = [&] {
+    U x;
+    x.q = wfrom + 32 * at_i;
+    x.qp = q_base + (long long)at_g * a.q.head + (long long)x.q * qc.stride;
+    x.dp = d_base + (long long)at_g * a.dout.head + (long long)x.q * dc.stride;
+    x.st = s_base + ((long long)at_g * a.lse_rows + x.q) * 4;
+    return x;
+  };
+  auto advance = [&] {  // by NW units, not behind the last one of the part
+    at_i += NW;
+    while (at_i >= wn) at_i -= wn, ++at_g;
+  };
+  auto copy_q = [&](const U& x, int stage) {
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    qc.all(x.qp, lds0 + stage * HALF, l, nq - x.q);
+  };
+  auto copy_d = [&](const U& x, int stage) {
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    dc.all(x.dp, lds0 + (2 + stage) * HALF, l, nq - x.q);
+  };
+  auto copy_terms = [&](const U& x, int stage) {
+    const unsigned off = nq - x.q >= 32 ? term_off : (unsigned)min(lane & 31, nq - x.q - 1) * 4u + (lane < 32 ? 0u : plane);
+    lds_dma4<4>(x.st, off, terms0 + stage * 256u);
+  };
+
+  f32x16 dk[DVB][2], dv[DVB][2];
+  float nil = 0.f;
+  asm volatile("" : "+v"(nil));
 #pragma unroll
   for (int x = 0; x < DVB; ++x)
 #pragma unroll
-    for (int t = 0; t < KT; ++t) dk[x][t] = dv[x][t] = zero16;
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) dk[x][t][i] = nil, dv[x][t][i] = nil;
+      pin_acc<D>(dk[x][t]);
+      pin_acc<D>(dv[x][t]);
+    }
   const float sl2 = a.scale * kLog2e;
   const int lane_a = TL::rowmajor_lane(0, lane);
   int b0, b1;
   TL::transposed_lane(0, lane, b0, b1);
 
-  if (nu > 0) copy(0, 0);
-  for (int u = 0; u < nu; ++u) {
-    const int par = u & 1;
-    if (u + 1 < nu) {
-      copy(u + 1, 1 - par);
-      win_wait<2 * NC + 1>();
-    } else {
-      win_wait<0>();
-    }
-    const unsigned char *qs = mine + par * HALF, *ds = mine + (2 + par) * HALF;
-    const int i0 = wave + NW * u, q0 = walk.from + (i0 % walk.n) * 32;
-    const long long pos = (long long)q0 + shift;
-    const bool masked = pos < walk.seen_from || pos + 32 > walk.seen_to || q0 + 32 > sq.n;
-    uint32_t pw[KT][8], sw[KT][8];
-    f32x16 s[KT], p[KT];
+  f32x16 S[2], dp[2];
+  uint32_t pw[2][2][4], sw[2][2][4];
+  auto place = [](int it, int& t, int& e) { t = (it >> 2) & 1, e = 8 * (it >> 3) + 2 * (it & 3); };
+  // P in place of S, dS in place of dP; slot n: the first operation of item n, the next of the one before, ...
+  auto p_slots = [&](int from_slot, int to_slot) {
 #pragma unroll
-    for (int st = 0; st < KS; ++st) {
-      const bf16x8 qa = TL::rowmajor_at(qs, lane_a, st), da = TL::rowmajor_at(ds, lane_a, st);
-#pragma unroll
-      for (int t = 0; t < KT; ++t) {
-        s[t] = mm32<F16>(qa, kreg[t][st], st == 0 ? zero16 : s[t]);
-        p[t] = mm32<F16>(da, vreg[t][st], st == 0 ? zero16 : p[t]);
+    for (int n = from_slot; n < to_slot; ++n) {
+      int t, e;
+      if (n < 16) {
+        place(n, t, e);
+        for (int i = 0; i < 2; ++i) {
+          S[t][e + i] *= sl2;
+          asm volatile("" : : "v"(S[t][e + i]));
+        }
+      }
+      if (n > 0 && n < 17) {
+        place(n - 1, t, e);
+        for (int i = 0; i < 2; ++i) {
+          S[t][e + i] = fast_exp2(S[t][e + i]);
+          asm volatile("" : : "v"(S[t][e + i]));
+        }
+      }
+      if (n > 1 && n < 18) {
+        place(n - 2, t, e);
+        pw[t][(n - 2) >> 3][(n - 2) & 3] = pack16<F16>(S[t][e], S[t][e + 1]);
+        asm volatile("" : : "v"(pw[t][(n - 2) >> 3][(n - 2) & 3]));
       }
     }
+  };
+  auto d_slots = [&](int from_slot, int to_slot) {
+#pragma unroll
+    for (int n = from_slot; n < to_slot; ++n) {
+      int t, e;
+      if (n < 16) {
+        place(n, t, e);
+        for (int i = 0; i < 2; ++i) {
+          dp[t][e + i] *= S[t][e + i];
+          asm volatile("" : : "v"(dp[t][e + i]));
+        }
+      }
+      if (n > 0 && n < 17) {
+        place(n - 1, t, e);
+        sw[t][(n - 1) >> 3][(n - 1) & 3] = pack16<F16>(dp[t][e], dp[t][e + 1]);
+        asm volatile("" : : "v"(sw[t][(n - 1) >> 3][(n - 1) & 3]));
+      }
+    }
+  };
+  auto word4 = [](const uint32_t (&w)[4]) { return __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3])); };
+  auto term16 = [&](int par, int which) {  // rows 8 * r4 + 4 h ..
+    f32x16 x;
 #pragma unroll
     for (int r4 = 0; r4 < 4; ++r4) {
-      const float4 x = *(const float4*)&stat_stage[wave][par][8 * r4 + 4 * h], y = *(const float4*)&stat_stage[wave][par][8 * r4 + 4 * h + 2];
-      const float lse2[4] = {x.x, x.z, y.x, y.z}, delta[4] = {x.y, x.w, y.y, y.w};
-#pragma unroll
-      for (int t = 0; t < KT; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = 4 * r4 + e;
-          s[t][i] = fast_exp2(fmaf(s[t][i], sl2, -lse2[e]));
-          p[t][i] = s[t][i] * (p[t][i] - delta[e]);
-        }
+      const f32x4 y = *(const f32x4*)&terms[wave][par][32 * which + 8 * r4 + 4 * h];
+      x[4 * r4] = y[0], x[4 * r4 + 1] = y[1], x[4 * r4 + 2] = y[2], x[4 * r4 + 3] = y[3];
     }
-    if (masked) {
+    return x;
+  };
+  U cur = {}, n1 = {}, n2 = {};
+  bf16x8 qcur[kAhead];
+  if (nu > 0) {
+    unit_at(begin + wave);
+    cur = unit_here();
+    if (nu > 1) advance();
+    n1 = unit_here();
+    copy_d(cur, 0);
+    copy_q(cur, 0);
+    copy_terms(cur, 0);
+    copy_d(n1, 1);
+    win_wait<NC>();
 #pragma unroll
-      for (int t = 0; t < KT; ++t)
+    for (int s = 0; s < kAhead; ++s) qcur[s] = TL::rowmajor_at(mine, lane_a, s);
+  }
+  // STEADY: the copies are of 32 rows that are there, piece by piece; else at once, and u may be the last unit.  `par` = u & 1 (a
+  // constant in the unrolled loop).
+  auto body = [&](auto steady_tag, int par, int u) {
+    constexpr bool STEADY = decltype(steady_tag)::value;
+    const bool more = STEADY || u + 1 < nu;
+    const unsigned char *qs = mine + par * HALF, *ds = mine + (2 + par) * HALF;
+    bf16x8 qr[KS], dr[KS], vr[KS], tr[KS], tq[KS];
+    int lane_v = lane_a;
+    asm volatile("" : "+v"(lane_v));  // (the addresses of V are made per unit: registers are short)
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) qr[s] = qcur[s];
+    if (!STEADY && more) copy_q(n1, 1 - par);
+    if (more) copy_terms(n1, 1 - par);
+    const f32x16 s_from = term16(par, 0);
+    f32x16 d_from;
+    __builtin_amdgcn_sched_barrier(0);
+    in_steps<PH>([&](auto number) {  // S
+      constexpr int j = decltype(number)::value, s = j >> 1;
+      constexpr bool copies = STEADY && j % kEvery == 0;
+      if (copies) {
+        qc.aim(lds0 + (1 - par) * HALF, j / kEvery);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (j == 0) mm_v<D, F16, true>(S[0], qr[0], kreg[0][0], s_from);
+      else {
+        if (j == 1) S[1] = s_from;  // (in place)
+        mm_v<D, F16, false>(S[j & 1], qr[s], kreg[j & 1][s], S[j & 1]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (copies) qc.piece(n1.qp, j / kEvery);
+      if (j == 1 && more) {
+        if (u + 2 < nu) advance();
+        n2 = unit_here();
+      }
+      if (j % 2 == 0) {
+        constexpr int to = s + kAhead;
+        if constexpr (to < KS) qr[to] = TL::rowmajor_at(qs, lane_a, to);
+        else dr[to - KS] = TL::rowmajor_at(ds, lane_a, to - KS);
+      }
+      if (j == PH - 5) d_from = term16(par, 1);
+      if constexpr (j % 2 && j >= PH - 4) vr[(j - PH + 4) / 2] = TL::rowmajor_at(vsecond, lane_v, (j - PH + 4) / 2);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (__builtin_expect(cur.q < seen_from || cur.q + 32 > seen_to, 0)) {  // (rows behind the last query among them)
+      int first = 4 * h;
+      asm volatile("" : "+v"(first));
+      first += cur.q;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int2 by = seen_by[wave][32 * t + l32];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int q = q0 + 8 * (i >> 2) + 4 * h + (i & 3);
-          const bool see = q >= from[t] && q < to[t];
-          s[t][i] = see ? s[t][i] : 0.f;
-          p[t][i] = see ? p[t][i] : 0.f;
-        }
-    }
-#pragma unroll
-    for (int t = 0; t < KT; ++t)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        pw[t][i] = pack16<F16>(s[t][2 * i], s[t][2 * i + 1]);
-        sw[t][i] = pack16<F16>(p[t][2 * i], p[t][2 * i + 1]);
-      }
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      bf16x8 po[KT], so[KT];
-#pragma unroll
-      for (int t = 0; t < KT; ++t) {
-        po[t] = __builtin_bit_cast(bf16x8, make_uint4(pw[t][4 * st], pw[t][4 * st + 1], pw[t][4 * st + 2], pw[t][4 * st + 3]));
-        so[t] = __builtin_bit_cast(bf16x8, make_uint4(sw[t][4 * st], sw[t][4 * st + 1], sw[t][4 * st + 2], sw[t][4 * st + 3]));
-      }
-#pragma unroll
-      for (int x = 0; x < DVB; ++x) {
-        const bf16x8 da = TL::transposed_at(ds, b0, b1, st, x), qa = TL::transposed_at(qs, b0, b1, st, x);
-#pragma unroll
-        for (int t = 0; t < KT; ++t) {
-          dv[x][t] = mm32<F16>(da, po[t], dv[x][t]);
-          dk[x][t] = mm32<F16>(qa, so[t], dk[x][t]);
+          const int q = first + 8 * (i >> 2) + (i & 3);
+          S[t][i] = q >= by.x && q < by.y ? S[t][i] : -INFINITY;
         }
       }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
+    auto dt_op = [&](int i) { return TL::transposed_at(ds, b0, b1, i / DVB, i % DVB); };
+    auto qt_op = [&](int i) { return TL::transposed_at(qs, b0, b1, i / DVB, i % DVB); };
+    constexpr int kP = 14;  // slots of P done behind dP: those of contraction step 0 among them
+    in_steps<PH>([&](auto number) {  // dP
+      constexpr int j = decltype(number)::value, s = j >> 1;
+      if constexpr (j == 0) mm_v<D, F16, true>(dp[0], dr[0], vreg[0], d_from);
+      else {
+        if (j == 1) dp[1] = d_from;
+        mm_v<D, F16, false>(dp[j & 1], dr[s], j & 1 ? vr[s] : vreg[s], dp[j & 1]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (j % 2 == 0) {
+        constexpr int to = s + kAhead;
+        if constexpr (to < KS) dr[to] = TL::rowmajor_at(ds, lane_a, to);
+        else tr[to - KS] = dt_op(to - KS);
+      } else if constexpr (s + 2 < KS) {
+        vr[s + 2] = TL::rowmajor_at(vsecond, lane_v, s + 2);
+      }
+      p_slots(kP * j / PH, kP * (j + 1) / PH);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    asm volatile("s_nop 1");
+    in_steps<PH>([&](auto number) {  // dV
+      constexpr int j = decltype(number)::value, i = j >> 1;
+      mm_acc<D, F16>(dv[i % DVB][j & 1], tr[i], word4(pw[j & 1][i / DVB]));
+      __builtin_amdgcn_sched_barrier(0);
+      if (j % 2 == 0) {
+        constexpr int to = i + kAhead;
+        if constexpr (to < KS) tr[to] = dt_op(to);
+        else tq[to - KS] = qt_op(to - KS);
+      }
+      constexpr int half = PH / 2 - 2;  // P of contraction step 1 is there two matrix instructions ahead of its use
+      if (j < half) p_slots(kP + (18 - kP) * j / half, kP + (18 - kP) * (j + 1) / half);
+      constexpr int d0 = j < 2 ? 0 : 14 * (j - 2) / (PH - 2), d1 = j < 2 ? 0 : 14 * (j - 1) / (PH - 2);
+      d_slots(d0, d1);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (!STEADY && more) copy_d(n2, par);
+    asm volatile("s_nop 1");
+    in_steps<PH>([&](auto number) {  // dK
+      constexpr int j = decltype(number)::value, i = j >> 1;
+      constexpr bool copies = STEADY && j % kEvery == 0;
+      if (copies) {
+        dc.aim(lds0 + (2 + par) * HALF, j / kEvery);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      mm_acc<D, F16>(dk[i % DVB][j & 1], tq[i], word4(sw[j & 1][i / DVB]));
+      __builtin_amdgcn_sched_barrier(0);
+      if (copies) dc.piece(n2.dp, j / kEvery);
+      if (more && j == PH - 2 * kAhead) {  // Q(u + 1) and all that is older have landed; newer: what has been requested of dO(u + 2)
+        constexpr int done = STEADY ? j / kEvery + 1 : NC;
+        win_wait<done>();
+      }
+      if (j % 2 == 0) {
+        constexpr int to = i + kAhead;
+        if constexpr (to < KS) tq[to] = qt_op(to);
+        else if (more) qcur[to - KS] = TL::rowmajor_at(mine + (1 - par) * HALF, lane_a, to - KS);
+      }
+      constexpr int half = PH / 2 - 2;
+      if (j < half) d_slots(14 + 3 * j / half, 14 + 3 * (j + 1) / half);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (D == 128 && !STEADY) mfma_fence();
+    cur = n1;
+    n1 = n2;
+  };
+  if (nu > 0) {
+    // (the next unit, and the one behind it; a walk that ends behind the last query ends in rows that are not there)
+    const bool plain = qc.plain(32) && dc.plain(32) && wfrom + 32 * wn <= nq;
+    int u = 0;
+    for (; plain && u + 3 < nu; u += 2) {
+      body(std::true_type{}, 0, u);
+      body(std::true_type{}, 1, u + 1);
+    }
+    if (D == 128) mfma_fence();
+    for (; u < nu; ++u) body(std::false_type{}, u & 1, u);
+    win_wait<0>();
   }
+  mfma_fence();
+#pragma unroll
+  for (int x = 0; x < DVB; ++x) pin_acc<D>(dk[x][0]), pin_acc<D>(dk[x][1]), pin_acc<D>(dv[x][0]), pin_acc<D>(dv[x][1]);
+  __builtin_amdgcn_sched_barrier(0);
   if (NW > 1) __syncthreads();
-  store_columns<D, F16, NW, KT>(dv, 1.f, (float*)smem, tid, keys, [&](int r) { return a.dv.out(b, sk.row0 + k0 + r, hk); });
-  if (NW > 1) __syncthreads();
-  else __builtin_amdgcn_wave_barrier();
-  store_columns<D, F16, NW, KT>(dk, a.scale, (float*)smem, tid, keys, [&](int r) { return a.dk.out(b, sk.row0 + k0 + r, hk); });
+  if (live == 1) {
+    store_columns<D, F16, NW, 2>(dv, 1.f, (float*)smem, PLACE / 4, tid, keys, [&](int r) { return a.dv.out(b, sk.row0 + k0 + r, hk); });
+    if (NW > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
+    store_columns<D, F16, NW, 2>(dk, a.scale, (float*)smem, PLACE / 4, tid, keys, [&](int r) { return a.dk.out(b, sk.row0 + k0 + r, hk); });
+  } else {
+    float* const slot = parts + (((long long)b * a.Hkv + hk) * plan.slots + plan.slot(kblk, part)) * (2 * 64 * D);
+    store_part<D, NW>(dv, (float*)smem, tid, keys, slot);
+    if (NW > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
+    store_part<D, NW>(dk, (float*)smem, tid, keys, slot + 64 * D);
+  }
+}
+
+// the parts of a block added in order, 8 elements a thread
+template <int D, bool F16>
+__global__ __launch_bounds__(256) void k_window_join(WinArgs a, DkvPlan plan, const float* __restrict__ parts, int blocks) {
+  const int block = blockIdx.x % blocks, bh = blockIdx.x / blocks, hk = bh % a.Hkv, b = bh / a.Hkv;
+  const WinSeq sq = win_seq(a.rq, b), sk = win_seq(a.rk, b);
+  const int k0 = block * 64, keys = min(64, sk.n - k0);
+  if (keys <= 0) return;
+  const KeyWalk walk(a.mask, k0, k0 + keys, sq.n, sk.n - sq.n, 32);
+  const int live = plan.live(walk.n * a.G, block < plan.sink_blocks ? plan.sink_parts : plan.parts);
+  if (live == 1) return;
+  const float* from = parts + (((long long)b * a.Hkv + hk) * plan.slots + plan.slot(block, 0)) * (2 * 64 * D);
+  for (int it = threadIdx.x; it < 2 * keys * (D / 8); it += 256) {
+    const int which = it / (keys * (D / 8)), r = it / (D / 8) % keys, ch = it % (D / 8);
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const float* x = from + which * 64 * D + r * D + ch * 8;
+    for (int p = 0; p < live; ++p, x += 2 * 64 * D) {
+      const float4 y0 = *(const float4*)x, y1 = *(const float4*)(x + 4);
+      v[0] += y0.x, v[1] += y0.y, v[2] += y0.z, v[3] += y0.w, v[4] += y1.x, v[5] += y1.y, v[6] += y1.z, v[7] += y1.w;
+    }
+    if (which) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= a.scale;
+    }
+    const uint4 u = {pack16<F16>(v[0], v[1]), pack16<F16>(v[2], v[3]), pack16<F16>(v[4], v[5]), pack16<F16>(v[6], v[7])};
+    *((uint4*)(which ? a.dk : a.dv).out(b, sk.row0 + k0 + r, hk) + ch) = u;
+  }
 }
 
 namespace {
 template <int D, bool F16>
-hipError_t launch(const WinArgs& a, hipStream_t s) {
+hipError_t launch(const WinArgs& a, float* parts, hipStream_t s) {
   const long long lanes = a.lse_rows * a.H * (D / 8);
   if (lanes > 0) k_window_stats<D, F16><<<(unsigned)((lanes + 255) / 256), 256, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int nqb = (a.rq.most + 63) / 64, per = 32 * dkv_tiles<D>(), nkb = (a.rk.most + per - 1) / per;
+  const int nqb = (a.rq.most + 63) / 64;
   const int chunked = a.mask.left >= 0;
   if (nqb > 0) {
     const unsigned items = (unsigned)nqb * a.H, grid = win_grid(a.B, items);
@@ -358,19 +889,24 @@ hipError_t launch(const WinArgs& a, hipStream_t s) {
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (nkb > 0) {
-    const unsigned items = (unsigned)nkb * a.Hkv, grid = win_grid(a.B, items);
-    if ((long long)items * a.B <= 512) k_window_dkv<D, F16, 4><<<grid, 256, 0, s>>>(a, items, nkb, chunked);
-    else k_window_dkv<D, F16, 1><<<grid, 64, 0, s>>>(a, items, nkb, chunked);
+  if (a.rk.most > 0) {
+    const DkvPlan plan = dkv_plan(a);
+    const unsigned items = (unsigned)plan.items() * a.Hkv, grid = win_grid(a.B, items);
+    if ((long long)items * a.B <= 256) k_window_dkv<D, F16, 4><<<grid, 256, 0, s>>>(a, plan, parts, items, chunked);
+    else k_window_dkv<D, F16, 2><<<grid, 128, 0, s>>>(a, plan, parts, items, chunked);
+    e = hipGetLastError();
+    if (e != hipSuccess || plan.slots == 0) return e;
+    const int blocks = plan.parts > 1 ? plan.nkb : plan.sink_blocks;
+    k_window_join<D, F16><<<(unsigned)(blocks * a.B * a.Hkv), 256, 0, s>>>(a, plan, parts, blocks);
     e = hipGetLastError();
   }
   return e;
 }
 }  // namespace
 
-hipError_t launch_window_bwd(const WinArgs& a, int d, bool f16, hipStream_t s) {
-  if (d == 128) return f16 ? launch<128, true>(a, s) : launch<128, false>(a, s);
-  return f16 ? launch<64, true>(a, s) : launch<64, false>(a, s);
+hipError_t launch_window_bwd(const WinArgs& a, int d, bool f16, float* parts, hipStream_t s) {
+  if (d == 128) return f16 ? launch<128, true>(a, parts, s) : launch<128, false>(a, parts, s);
+  return f16 ? launch<64, true>(a, parts, s) : launch<64, false>(a, parts, s);
 }
 
 }  // namespace vsa

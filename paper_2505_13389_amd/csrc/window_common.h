@@ -147,7 +147,7 @@ struct WinArgs {
   WinRows rq, rk;
   RowView q, k, v, o, dout, dq, dk, dv;
   float* lse;    // [H, lse_rows]
-  float2* stats;  // [H, lse_rows], of the backward: lse in log2 units (+inf for a row that sees nothing), rowsum(dO * O)
+  float* stats;  // [2][H, lse_rows], of the backward: -lse / scale (-inf for a row that sees nothing), -rowsum(dO * O)
   long long lse_rows;
   float scale;
   // row of the statistics of query i of sequence b with first row row0

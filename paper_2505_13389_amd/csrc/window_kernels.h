@@ -24,7 +24,9 @@ struct AppendArgs {
 };
 
 hipError_t launch_window_fwd(const WinArgs& a, int d, bool f16, hipStream_t s);
-hipError_t launch_window_bwd(const WinArgs& a, int d, bool f16, hipStream_t s);
+// `parts`: window_parts(a, d) floats
+hipError_t launch_window_bwd(const WinArgs& a, int d, bool f16, float* parts, hipStream_t s);
+size_t window_parts(const WinArgs& a, int d);
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
 // many rows a key head: the walk of launch_window_fwd over pages
 hipError_t launch_cache_chunk(const WinArgs& a, const CacheArgs& c, int d, bool f16, hipStream_t s);
