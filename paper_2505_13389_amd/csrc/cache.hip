@@ -31,14 +31,12 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t u, float f) {
 __device__ __forceinline__ float finite_or_nan(float x) { return x - x == 0.f ? x : __uint_as_float(0x7fc00000u); }
 
 template <int D, bool F16>
-__global__ __launch_bounds__(2 * D) void k_cache_append(AppendArgs a, unsigned items, int most_pages) {
+__global__ __launch_bounds__(2 * D) void k_cache_append(AppendArgs a, int most_pages) {
   constexpr int CPR = D / 8, NT = 2 * D, NWV = NT / 64;
   __shared__ float top_of[2][NWV];
   __shared__ uint32_t tile[D * 16];  // V: [dv][16 dwords of 4 tokens], 16-byte chunks swizzled
-  int b;
-  unsigned item;
-  if (!win_item(blockIdx.x, items, false, b, item)) return;
-  const int head = (int)(item % (unsigned)a.Hkv), slot_page = (int)(item / (unsigned)a.Hkv);
+  const int head = (int)(blockIdx.x % (unsigned)a.Hkv), rest = (int)(blockIdx.x / (unsigned)a.Hkv);  // (rows of all heads lie side by side)
+  const int slot_page = rest % most_pages, b = rest / most_pages;
   const WinSeq seq = win_seq(a.rows, b);
   const int start = max(0, min(a.c.lens[b], a.c.max_pages * kPage));
   const int page = start / kPage + slot_page;
@@ -141,13 +139,13 @@ __global__ __launch_bounds__(2 * D) void k_cache_append(AppendArgs a, unsigned i
 
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s) {
   const int most_pages = (a.rows.most + kPage - 1) / kPage + 1;
-  const unsigned items = (unsigned)most_pages * (unsigned)a.Hkv, grid = win_grid(a.B, items);
+  const unsigned grid = (unsigned)a.B * (unsigned)most_pages * (unsigned)a.Hkv;
   if (a.d == 128) {
-    if (a.f16) k_cache_append<128, true><<<grid, 256, 0, s>>>(a, items, most_pages);
-    else k_cache_append<128, false><<<grid, 256, 0, s>>>(a, items, most_pages);
+    if (a.f16) k_cache_append<128, true><<<grid, 256, 0, s>>>(a, most_pages);
+    else k_cache_append<128, false><<<grid, 256, 0, s>>>(a, most_pages);
   } else {
-    if (a.f16) k_cache_append<64, true><<<grid, 128, 0, s>>>(a, items, most_pages);
-    else k_cache_append<64, false><<<grid, 128, 0, s>>>(a, items, most_pages);
+    if (a.f16) k_cache_append<64, true><<<grid, 128, 0, s>>>(a, most_pages);
+    else k_cache_append<64, false><<<grid, 128, 0, s>>>(a, most_pages);
   }
   return hipGetLastError();
 }

@@ -159,17 +159,15 @@ __device__ __forceinline__ void store_part(f32x16 (&acc)[D / 32][2], float* buf,
 //   dQ += K^T dS(u)    the first of P(u + 1), copies of V(u + 2)
 // K has three stages (of unit u to its end, of u + 1, of u + 2), V two.
 template <int D, bool F16, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, unsigned items, int nqb, int chunked) {
+__global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, int nqb) {
   using TL = Tile<D>;
   constexpr int KS = D / 16, DVB = D / 32, HALF = 32 * D * 2, NC = RowCopy<D>::NC, PH = 2 * KS, IPM = 16 / PH;  // softmax items a matrix instruction
   constexpr int kAhead = 2, kEvery = PH / NC, kEarly = 4;  // kEarly: items of P done in the phase before its own
   constexpr int STAGES = 5 * HALF, PLACE = STAGES > 64 * D * 4 ? STAGES : 64 * D * 4;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * PLACE];
-  int b;
-  unsigned item;
-  if (!win_item(blockIdx.x, items, chunked != 0, b, item)) return;
-  const int g = (int)(item % (unsigned)a.G), rest = (int)(item / (unsigned)a.G);
-  const int hk = rest / nqb, qb = chunked ? rest % nqb : nqb - 1 - rest % nqb, hq = hk * a.G + g;
+  int b, hk, item;
+  if (!win_item(blockIdx.x, (unsigned)a.Hkv, (unsigned)(nqb * a.G), b, hk, item)) return;
+  const int g = item % a.G, qb = nqb - 1 - item / a.G, hq = hk * a.G + g;  // (the last queries have most to walk: they come first)
   const WinSeq sq = win_seq(a.rq, b), sk = win_seq(a.rk, b);
   const int r0 = qb * 64, rows = min(64, sq.n - r0);
   if (rows <= 0) return;
@@ -500,7 +498,7 @@ size_t window_parts(const WinArgs& a, int d) { return (size_t)a.B * a.Hkv * dkv_
 //   dK += Q^T dS                    the rest of dS, copies of dO(u + 2)
 // dK and dV are accumulation registers, K and V of the first 32 keys ordinary ones, V of the others is in LDS.
 template <int D, bool F16, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan plan, float* __restrict__ parts, unsigned items, int chunked) {
+__global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan plan, float* __restrict__ parts) {
   using TL = Tile<D>;
   constexpr int KS = D / 16, DVB = D / 32, HALF = 32 * D * 2, NC = RowCopy<D>::NC, PH = 2 * KS;
   constexpr int kAhead = 2, kEvery = PH / NC;
@@ -510,12 +508,9 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
   __shared__ __attribute__((aligned(256))) float terms[NW][2][64];  // of a unit's 32 rows: what S starts from, dP
   __shared__ int2 seen_by[NW][64];  // queries that see a key (registers are short)
   static_assert(PLACE == 64 * D * 4, "the partial results fit the stages");
-  int b;
-  unsigned item;
-  if (!win_item(blockIdx.x, items, chunked != 0, b, item)) return;
-  const int per_head = plan.items(), hk = (int)(item / (unsigned)per_head);
-  int kblk, part, of;
-  plan.at((int)(item % (unsigned)per_head), kblk, part, of);
+  int b, hk, item, kblk, part, of;
+  if (!win_item(blockIdx.x, (unsigned)a.Hkv, (unsigned)plan.items(), b, hk, item)) return;
+  plan.at(item, kblk, part, of);
   const WinSeq sq = win_seq(a.rq, b), sk = win_seq(a.rk, b);
   const int k0 = kblk * 64, keys = min(64, sk.n - k0);
   if (keys <= 0) return;
@@ -881,19 +876,18 @@ hipError_t launch(const WinArgs& a, float* parts, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int nqb = (a.rq.most + 63) / 64;
-  const int chunked = a.mask.left >= 0;
   if (nqb > 0) {
     const unsigned items = (unsigned)nqb * a.H, grid = win_grid(a.B, items);
-    if ((long long)items * a.B <= 512) k_window_dq<D, F16, 4><<<grid, 256, 0, s>>>(a, items, nqb, chunked);
-    else k_window_dq<D, F16, 1><<<grid, 64, 0, s>>>(a, items, nqb, chunked);
+    if ((long long)items * a.B <= 512) k_window_dq<D, F16, 4><<<grid, 256, 0, s>>>(a, nqb);
+    else k_window_dq<D, F16, 1><<<grid, 64, 0, s>>>(a, nqb);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (a.rk.most > 0) {
     const DkvPlan plan = dkv_plan(a);
     const unsigned items = (unsigned)plan.items() * a.Hkv, grid = win_grid(a.B, items);
-    if ((long long)items * a.B <= 256) k_window_dkv<D, F16, 4><<<grid, 256, 0, s>>>(a, plan, parts, items, chunked);
-    else k_window_dkv<D, F16, 2><<<grid, 128, 0, s>>>(a, plan, parts, items, chunked);
+    if ((long long)items * a.B <= 256) k_window_dkv<D, F16, 4><<<grid, 256, 0, s>>>(a, plan, parts);
+    else k_window_dkv<D, F16, 2><<<grid, 128, 0, s>>>(a, plan, parts);
     e = hipGetLastError();
     if (e != hipSuccess || plan.slots == 0) return e;
     const int blocks = plan.parts > 1 ? plan.nkb : plan.sink_blocks;

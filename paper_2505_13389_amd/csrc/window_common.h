@@ -128,16 +128,25 @@ __host__ __device__ inline WinSeq win_seq(const WinRows& r, int b) {
   return {s, (int)(e - s)};
 }
 
-// Workgroup number -> (sequence, item) with `items` of a sequence padded up to a multiple of 8.
-// Workgroups are dealt to the 8 XCDs in turn.  `chunked`: an XCD takes a contiguous run of a sequence's items, so that
-// neighbours (the heads of a group, then the next queries), which read the same keys, find them in one L2; sequences may differ in
-// length, so the runs are of a sequence and not of the launch.  Otherwise in turn, for items of unequal work.
-__device__ __forceinline__ bool win_item(unsigned block, unsigned items, bool chunked, int& b, unsigned& item) {
-  const unsigned padded = (items + 7u) & ~7u;
+// Workgroup number -> sequence, key head and one of the head's `per_head` items (the items of a sequence padded up to a multiple of 8).
+// Workgroups are dealt to the 8 XCDs in turn, each of which has an L2.  An XCD takes whole heads, whose items read the same
+// keys; those of the heads left over are dealt to all of them, item by item, so that the XCDs get the same amount of work (16384
+// tokens, 12 heads, windows of four frames: with contiguous runs of all items a fifth of the chip's time was lost).
+__device__ __forceinline__ bool win_item(unsigned block, unsigned heads, unsigned per_head, int& b, int& head, int& item) {
+  const unsigned padded = (heads * per_head + 7u) & ~7u;
   b = (int)(block / padded);
-  const unsigned i = block - (unsigned)b * padded, per = padded >> 3;
-  item = chunked ? (i & 7u) * per + (i >> 3) : i;
-  return item < items;
+  const unsigned i = block - (unsigned)b * padded, x = i & 7u, n = i >> 3, whole = heads >> 3, rest = heads & 7u;
+  if (n < whole * per_head) {
+    const unsigned k = n / per_head;
+    head = (int)(x + 8u * k);
+    item = (int)(n - k * per_head);
+    return true;
+  }
+  const unsigned j = (n - whole * per_head) * 8u + x;
+  if (j >= rest * per_head) return false;
+  item = (int)(j / rest);
+  head = (int)(8u * whole + j - (unsigned)item * rest);
+  return true;
 }
 inline unsigned win_grid(int B, unsigned items) { return (unsigned)B * ((items + 7u) & ~7u); }
 

@@ -126,7 +126,7 @@ __device__ __forceinline__ void mm_o(f32x16& acc, bf16x8 a, bf16x8 b) {
 }
 
 template <int D, bool F16, int NW, bool PAGED>
-__global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs cache, unsigned items, int nqb, int chunked) {
+__global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs cache, int nqb) {
   using TL = Tile<D>;
   using TK = WinTicks<D, PAGED>;
   constexpr TK ticks;
@@ -135,11 +135,9 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
   __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * 4 * HALF];
   __shared__ float ml[NW * 64 * 2];
 
-  int b;
-  unsigned item;
-  if (!win_item(blockIdx.x, items, chunked != 0, b, item)) return;
-  const int g = (int)(item % (unsigned)a.G), rest = (int)(item / (unsigned)a.G);
-  const int hk = rest / nqb, qb = chunked ? rest % nqb : nqb - 1 - rest % nqb, hq = hk * a.G + g;
+  int b, hk, item;
+  if (!win_item(blockIdx.x, (unsigned)a.Hkv, (unsigned)(nqb * a.G), b, hk, item)) return;
+  const int g = item % a.G, qb = nqb - 1 - item / a.G, hq = hk * a.G + g;  // (the last queries have most to walk: they come first)
   const WinSeq sq = win_seq(a.rq, b);
   const int r0 = qb * 64, rows = min(64, sq.n - r0);
   if (rows <= 0) return;
@@ -609,10 +607,9 @@ template <int D, bool F16, bool PAGED>
 hipError_t launch(const WinArgs& a, const CacheArgs& c, hipStream_t s) {
   const int nqb = (a.rq.most + 63) / 64;
   const unsigned items = (unsigned)nqb * (unsigned)a.H, grid = win_grid(a.B, items);
-  const int chunked = a.mask.left >= 0;
   const long long blocks = (long long)items * a.B;
-  if (blocks <= 512) k_window_fwd<D, F16, 4, PAGED><<<grid, 256, 0, s>>>(a, c, items, nqb, chunked);
-  else k_window_fwd<D, F16, 1, PAGED><<<grid, 64, 0, s>>>(a, c, items, nqb, chunked);
+  if (blocks <= 512) k_window_fwd<D, F16, 4, PAGED><<<grid, 256, 0, s>>>(a, c, nqb);
+  else k_window_fwd<D, F16, 1, PAGED><<<grid, 64, 0, s>>>(a, c, nqb);
   return hipGetLastError();
 }
 }  // namespace
