@@ -14,14 +14,15 @@ call, unless a workspace is handed over.
     out = cache.attend(q, table, lens_now, left=6, right=0, sinks=1, unit=1560)
 """
 import ctypes as C
-from contextlib import nullcontext
 from dataclasses import dataclass
 
 import torch
 
-from .vsa import VsaError, _p, lib
+from .vsa import VsaError, lib
 
 PAGE = 64
+# the current stream's handle, without the object around it where torch offers that
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 
 
@@ -89,27 +90,61 @@ def _whole(t, name, shape, dtype, device):
     return t
 
 
-def _on(device):
-    """The device's context and its current stream."""
-    if device.type != "cuda":
-        raise ValueError(f"tensors must be on a GPU, not on {device}")
-    here = device.index is None or device.index == torch.cuda.current_device()
-    return (nullcontext() if here else torch.cuda.device(device)), C.c_void_p(torch.cuda.current_stream(device).cuda_stream)
-
-
 def _shapes(pb, packed):
     if packed:
         return (pb.total_q, pb.H, pb.d), (pb.total_k, pb.Hkv, pb.d)
     return (pb.B, pb.max_q, pb.H, pb.d), (pb.B, pb.max_k, pb.Hkv, pb.d)
 
 
-def _offsets(pb, cu_q, cu_k, device):
+def _run(device, name, *args):
+    """The entry point `name` on the device's current stream."""
+    index = device.index
+    if index is None:
+        raise ValueError(f"tensors must be on a GPU, not on {device}")
+    f = getattr(lib(), name)
+    if index == torch.cuda.current_device():
+        rc = f(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            rc = f(*args, _raw_stream(index))
+    if rc:
+        raise VsaError(name, rc)
+
+
+_known = {}  # parameters of calls by their shapes, strides, types and mask: building them takes longer than a launch
+_NAMES = ("q", "k", "v", "out", "dout", "dq", "dk", "dv")
+
+
+def _window_call(pb, tensors, lse, cu_q, cu_k):
+    """Address of the parameters of a call, its tensors checked: q, k, v, out and, backward, dout, dq, dk, dv."""
+    q = tensors[0]
+    device = q.device
     if (cu_q is None) != (cu_k is None):
         raise ValueError("cu_q and cu_k: both or neither")
-    if cu_q is not None:
+    packed = cu_q is not None
+    key = (*pb.__dict__.values(), packed, *[x for t in tensors for x in (t.shape, t.stride())])
+    known = _known.get(key)
+    if known is None:
+        sq, sk = _shapes(pb, packed)
+        p = pb.params()
+        for n, t in zip(_NAMES, tensors):
+            setattr(p, n, _strides(_want(t, n, sk if n in ("k", "v", "dk", "dv") else sq, pb.dtype, device), n))
+        if len(_known) >= 1024:
+            _known.clear()
+        known = _known[key] = (p, C.addressof(p), (pb.H, sq[0] if packed else sq[0] * sq[1]), int(lib().vsa_window_workspace_bytes(C.byref(p))))
+    for n, t in zip(_NAMES, tensors):
+        if t.dtype is not pb.dtype or t.device != device:
+            raise ValueError(f"{n} must be {pb.dtype} on {device}, not {t.dtype} on {t.device}")
+    if packed:
         _whole(cu_q, "cu_q", (pb.B + 1,), torch.int32, device)
         _whole(cu_k, "cu_k", (pb.B + 1,), torch.int32, device)
-    return cu_q is not None
+    if lse is not None:
+        _whole(lse, "lse", known[2], torch.float32, device)
+    return known
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def vsa_window_workspace_bytes(pb: WindowProblem) -> int:
@@ -118,37 +153,18 @@ def vsa_window_workspace_bytes(pb: WindowProblem) -> int:
 
 def vsa_window_forward(pb: WindowProblem, q, k, v, out, lse=None, cu_q=None, cu_k=None):
     """out, lse (or None: not wanted) are written; lse is fp32 [H, rows]."""
-    device, packed = q.device, _offsets(pb, cu_q, cu_k, q.device)
-    sq, sk = _shapes(pb, packed)
-    p = pb.params()
-    for n, t, s in (("q", q, sq), ("k", k, sk), ("v", v, sk), ("out", out, sq)):
-        setattr(p, n, _strides(_want(t, n, s, pb.dtype, device), n))
-    if lse is not None:
-        _whole(lse, "lse", (pb.H, sq[0] if packed else sq[0] * sq[1]), torch.float32, device)
-    context, stream = _on(device)
-    with context:
-        rc = lib().vsa_window_forward(C.byref(p), _p(q), _p(k), _p(v), _p(cu_q), _p(cu_k), _p(out), _p(lse), stream)
-    if rc:
-        raise VsaError("vsa_window_forward", rc)
+    call = _window_call(pb, (q, k, v, out), lse, cu_q, cu_k)
+    _run(q.device, "vsa_window_forward", call[1], q.data_ptr(), k.data_ptr(), v.data_ptr(), _at(cu_q), _at(cu_k), out.data_ptr(), _at(lse))
 
 
 def vsa_window_backward(pb: WindowProblem, q, k, v, out, dout, lse, dq, dk, dv, workspace, cu_q=None, cu_k=None):
     """dq, dk, dv are written; out, lse as the forward wrote them."""
-    device, packed = q.device, _offsets(pb, cu_q, cu_k, q.device)
-    sq, sk = _shapes(pb, packed)
-    p = pb.params()
-    for n, t, s in (("q", q, sq), ("k", k, sk), ("v", v, sk), ("out", out, sq), ("dout", dout, sq), ("dq", dq, sq), ("dk", dk, sk),
-                    ("dv", dv, sk)):
-        setattr(p, n, _strides(_want(t, n, s, pb.dtype, device), n))
-    _whole(lse, "lse", (pb.H, sq[0] if packed else sq[0] * sq[1]), torch.float32, device)
-    if workspace is not None and workspace.device != device:
+    call = _window_call(pb, (q, k, v, out, dout, dq, dk, dv), lse, cu_q, cu_k)
+    if workspace is not None and workspace.device != q.device:
         raise ValueError("the workspace must be on the tensors' device")
-    context, stream = _on(device)
-    with context:
-        rc = lib().vsa_window_backward(C.byref(p), _p(q), _p(k), _p(v), _p(cu_q), _p(cu_k), _p(out), _p(dout), _p(lse), _p(dq), _p(dk),
-                                       _p(dv), _p(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), stream)
-    if rc:
-        raise VsaError("vsa_window_backward", rc)
+    _run(q.device, "vsa_window_backward", call[1], q.data_ptr(), k.data_ptr(), v.data_ptr(), _at(cu_q), _at(cu_k), out.data_ptr(),
+         dout.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _at(workspace),
+         0 if workspace is None else workspace.numel() * workspace.element_size())
 
 
 class WindowBuffers:
@@ -206,6 +222,8 @@ class PagedCache:
         _whole(v_scale, "v_scale", (pages, heads), torch.float32, k.device)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.pages, self.Hkv, self.d, self.device = pages, heads, d, k.device
+        self._pool = (k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self._params = {}  # of calls by their shapes, strides, types and mask: building them takes longer than the launch
 
     def _call(self, x, table, lens, cu, most, name):
         """The parameters of a call whose tokens are x: [B, n, heads, d], or packed [rows, heads, d] with offsets `cu`."""
@@ -216,62 +234,78 @@ class PagedCache:
         B = table.shape[0] if table.dim() == 2 else -1
         if B < 1:
             raise ValueError("table is int32 [B, max_pages]")
-        _whole(table, "table", (B, table.shape[1]), torch.int32, self.device)
-        _whole(lens, "lens", (B,), torch.int32, self.device)
+        if tuple(lens.shape) != (B,):
+            raise ValueError(f"lens is int32 [{B}], not {tuple(lens.shape)}")
         if cu is None:
             if x.shape[0] != B:
                 raise ValueError(f"{name} has {x.shape[0]} sequences, table has {B}")
             most, rows = x.shape[1], 0
         else:
-            _whole(cu, "cu", (B + 1,), torch.int32, self.device)
+            if tuple(cu.shape) != (B + 1,):
+                raise ValueError(f"cu is int32 [{B + 1}], not {tuple(cu.shape)}")
             rows = x.shape[0]
             most = rows if most is None else min(most, rows)
-        p = VsaCache(B=B, H=x.shape[-2], Hkv=self.Hkv, d=self.d, max_q=most, total_q=rows, pages=self.pages, max_pages=table.shape[1],
-                     unit=1, left=-1, right=0, dtype=_DTYPES[x.dtype])
-        return p, cu is not None
+        if len(self._params) >= 256:
+            self._params.clear()
+        return VsaCache(B=B, H=x.shape[-2], Hkv=self.Hkv, d=self.d, max_q=most, total_q=rows, pages=self.pages, max_pages=table.shape[1],
+                        unit=1, left=-1, right=0, dtype=_DTYPES[x.dtype])
+
+    def _check(self, tokens, table, lens, cu):
+        """What a call's tensors have to be besides their shapes and strides."""
+        here = self.device
+        for t in tokens:
+            if t.device != here:
+                raise ValueError(f"tensors must be on the cache's device, {here}, not on {t.device}")
+        for t in (table, lens) if cu is None else (table, lens, cu):
+            if t.dtype is not torch.int32 or not t.is_contiguous() or t.device != here:
+                raise ValueError(f"table, lens and cu are contiguous int32 tensors on {here}, not {t.dtype} on {t.device}")
 
     def append(self, k, v, table, lens, cu=None, max_new=None):
         """New tokens k, v behind the `lens` (int32 [B]) tokens that each sequence has: [B, n, Hkv, d], or packed
         [rows, Hkv, d] with offsets `cu` (int32 [B+1]) and at most `max_new` tokens a sequence (None: as many as there are rows)."""
-        p, _ = self._call(k, table, lens, cu, max_new, "k")
-        if k.shape[-2] != self.Hkv:
-            raise ValueError(f"k has {k.shape[-2]} heads, the cache has {self.Hkv}")
-        _want(k, "k", k.shape, k.dtype, self.device)
-        _want(v, "v", k.shape, k.dtype, self.device)
-        p.k, p.v = _strides(k, "k"), _strides(v, "v")
-        context, stream = _on(self.device)
-        with context:
-            rc = lib().vsa_cache_append(C.byref(p), _p(k), _p(v), _p(cu), _p(lens), _p(table), _p(self.k), _p(self.v), _p(self.k_scale),
-                                        _p(self.v_scale), stream)
-        if rc:
-            raise VsaError("vsa_cache_append", rc)
+        packed = cu is not None
+        key = (k.shape, k.stride(), v.shape, v.stride(), k.dtype, v.dtype, table.shape, lens.shape, packed and cu.shape, max_new)
+        known = self._params.get(key)
+        if known is None:
+            p = self._call(k, table, lens, cu, max_new, "k")
+            if k.shape[-2] != self.Hkv:
+                raise ValueError(f"k has {k.shape[-2]} heads, the cache has {self.Hkv}")
+            _want(v, "v", k.shape, k.dtype, v.device)
+            p.k, p.v = _strides(k, "k"), _strides(v, "v")
+            known = self._params[key] = (p, C.addressof(p))
+        self._check((k, v), table, lens, cu)
+        _run(self.device, "vsa_cache_append", known[1], k.data_ptr(), v.data_ptr(), cu.data_ptr() if packed else None, lens.data_ptr(), table.data_ptr(),
+                  *self._pool)
 
     def attend(self, q, table, lens, cu=None, max_q=None, *, left=-1, right=0, sinks=0, unit=1, softmax_scale=0.0, out=None, lse=None,
                workspace=None):
         """Attention of q over the first `lens` tokens of each sequence, of which the queries are the last: q [B, n, H, d], or packed
         [rows, H, d] with offsets `cu` and at most `max_q` queries a sequence.  Returns out (a new tensor, or the one given); rows
         that belong to no sequence are not written."""
-        p, packed = self._call(q, table, lens, cu, max_q, "q")
-        _want(q, "q", q.shape, q.dtype, self.device)
-        p.unit, p.left, p.right, p.sinks, p.softmax_scale = unit, left, right, sinks, softmax_scale
+        packed = cu is not None
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
-        else:
-            _want(out, "out", q.shape, q.dtype, self.device)
-        p.q, p.out = _strides(q, "q"), _strides(out, "out")
+        elif out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError(f"out must be {q.dtype} {tuple(q.shape)}, not {out.dtype} {tuple(out.shape)}")
+        key = (q.shape, q.stride(), out.stride(), q.dtype, table.shape, lens.shape, packed and cu.shape, max_q, left, right, sinks, unit,
+               softmax_scale)
+        known = self._params.get(key)
+        if known is None:
+            p = self._call(q, table, lens, cu, max_q, "q")
+            p.unit, p.left, p.right, p.sinks, p.softmax_scale = unit, left, right, sinks, softmax_scale
+            p.q, p.out = _strides(q, "q"), _strides(out, "out")
+            known = self._params[key] = (p, C.addressof(p), vsa_cache_workspace_bytes(p))
+        self._check((q, out), table, lens, cu)
         if lse is not None:
             _whole(lse, "lse", (q.shape[-2], q.shape[0] if packed else q.shape[0] * q.shape[1]), torch.float32, self.device)
-        context, stream = _on(self.device)
-        with context:
-            if workspace is None:
-                workspace = torch.empty(vsa_cache_workspace_bytes(p), dtype=torch.uint8, device=self.device)
-            elif workspace.device != self.device:
+        if workspace is None:
+            workspace, size = torch.empty(known[2], dtype=torch.uint8, device=self.device), known[2]
+        else:
+            if workspace.device != self.device:
                 raise ValueError("the workspace must be on the cache's device")
-            rc = lib().vsa_cache_attention(C.byref(p), _p(q), _p(cu), _p(lens), _p(table), _p(self.k), _p(self.v), _p(self.k_scale),
-                                           _p(self.v_scale), _p(out), _p(lse), _p(workspace),
-                                           workspace.numel() * workspace.element_size(), stream)
-        if rc:
-            raise VsaError("vsa_cache_attention", rc)
+            size = workspace.numel() * workspace.element_size()
+        _run(self.device, "vsa_cache_attention", known[1], q.data_ptr(), cu.data_ptr() if packed else None, lens.data_ptr(), table.data_ptr(), *self._pool,
+                  out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), size)
         return out
 
     def workspace_bytes(self, B, H, max_q, max_pages):
