@@ -28,14 +28,18 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t u, float f) {
   const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
   return to_e4m3(lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f);
 }
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ float finite_or_nan(float x) { return x - x == 0.f ? x : __uint_as_float(0x7fc00000u); }
 
-template <int D, bool F16>
+// LARGE: every XCD takes a contiguous run of the launch (pages and heads whose rows lie side by side), and what is written goes past the
+// caches: 75600 tokens, 40 heads, d = 128 454 -> LARGE_US us.
+template <int D, bool F16, bool LARGE>
 __global__ __launch_bounds__(2 * D) void k_cache_append(AppendArgs a, int most_pages) {
   constexpr int CPR = D / 8, NT = 2 * D, NWV = NT / 64;
   __shared__ float top_of[2][NWV];
   __shared__ uint32_t tile[D * 16];  // V: [dv][16 dwords of 4 tokens], 16-byte chunks swizzled
-  const int head = (int)(blockIdx.x % (unsigned)a.Hkv), rest = (int)(blockIdx.x / (unsigned)a.Hkv);  // (rows of all heads lie side by side)
+  const unsigned block = LARGE ? xcd_chunked_id(blockIdx.x, gridDim.x) : blockIdx.x;
+  const int head = (int)(block % (unsigned)a.Hkv), rest = (int)(block / (unsigned)a.Hkv);  // (rows of all heads lie side by side)
   const int slot_page = rest % most_pages, b = rest / most_pages;
   const WinSeq seq = win_seq(a.rows, b);
   const int start = max(0, min(a.c.lens[b], a.c.max_pages * kPage));
@@ -101,7 +105,9 @@ __global__ __launch_bounds__(2 * D) void k_cache_append(AppendArgs a, int most_p
     uint2* const p = (uint2*)(kp + slot * D) + c;
     if (slot >= lo && slot < hi) {
       const float* f = x[0][i];
-      *p = make_uint2(to_e4m3(f[0] * ik, f[1] * ik, f[2] * ik, f[3] * ik), to_e4m3(f[4] * ik, f[5] * ik, f[6] * ik, f[7] * ik));
+      const u32x2 u = {to_e4m3(f[0] * ik, f[1] * ik, f[2] * ik, f[3] * ik), to_e4m3(f[4] * ik, f[5] * ik, f[6] * ik, f[7] * ik)};
+      if (LARGE) __builtin_nontemporal_store(u, (u32x2*)p);
+      else *(u32x2*)p = u;
     } else if (slot < lo && ratio[0] != 1.f) {
       const uint2 u = *p;
       *p = make_uint2(rescaled(u.x, ratio[0]), rescaled(u.y, ratio[0]));
@@ -133,20 +139,27 @@ __global__ __launch_bounds__(2 * D) void k_cache_append(AppendArgs a, int most_p
       }
       u = make_uint4(n[0], n[1], n[2], n[3]);
     }
-    *p = u;
+    store16<LARGE>(p, u);
   }
 }
 
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s) {
   const int most_pages = (a.rows.most + kPage - 1) / kPage + 1;
   const unsigned grid = (unsigned)a.B * (unsigned)most_pages * (unsigned)a.Hkv;
+  const bool large = (a.rows.cu ? a.rows.total : (long long)a.B * a.rows.most) * a.Hkv * a.d * 4 > kStreamBytes;
+#define VSA_APPEND(D_, F16_)                                                            \
+  do {                                                                                  \
+    if (large) k_cache_append<D_, F16_, true><<<grid, 2 * D_, 0, s>>>(a, most_pages);   \
+    else k_cache_append<D_, F16_, false><<<grid, 2 * D_, 0, s>>>(a, most_pages);        \
+  } while (0)
   if (a.d == 128) {
-    if (a.f16) k_cache_append<128, true><<<grid, 256, 0, s>>>(a, most_pages);
-    else k_cache_append<128, false><<<grid, 256, 0, s>>>(a, most_pages);
+    if (a.f16) VSA_APPEND(128, true);
+    else VSA_APPEND(128, false);
   } else {
-    if (a.f16) k_cache_append<64, true><<<grid, 128, 0, s>>>(a, most_pages);
-    else k_cache_append<64, false><<<grid, 128, 0, s>>>(a, most_pages);
+    if (a.f16) VSA_APPEND(64, true);
+    else VSA_APPEND(64, false);
   }
+#undef VSA_APPEND
   return hipGetLastError();
 }
 
@@ -161,30 +174,103 @@ hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s) {
 // launch where there is more than one part.  Bound by HBM: 2 d bytes a token and head.
 constexpr float kNoRow = -1e30f;
 
+// How the pages are dealt to workgroups.  The host knows bounds only, so the kernels work it out from the lengths: all pages that the
+// sequences walk (times key heads and row tiles) over `target` workgroups give the pages of a part, a multiple of 4 (a workgroup's
+// wavefronts) and the same for all sequences; a sequence has as many parts as it needs.  Then all workgroups run side by side, take
+// about as long as each other, and none is launched for pages that are not there.
 struct TokenPlan {
-  int row_tiles, per_part, parts;  // pages of a part (a multiple of 4)
+  int target, groups, grid;  // workgroups aimed at; (sequence, key head, row tile) triples; workgroups needed at most
+  int one;           // every sequence has one part, whatever its length: nothing is joined
 };
-static TokenPlan token_plan(int B, int H, int Hkv, int max_q, int max_pages, const WinMask* m) {
-  TokenPlan p;
+static TokenPlan token_plan(int B, int H, int Hkv, int max_q, int max_pages) {
   const int G = H / Hkv;
-  p.row_tiles = (int)(((long long)max_q * G + 15) / 16);
-  long long pages = max_pages;
-  if (m && m->left >= 0) {  // what the queries of a tile can see at most
-    const long long sinks = ((long long)m->sinks * m->unit + kPage - 1) / kPage;
-    const long long run = m->right < 0 ? max_pages : ((long long)(m->left + 1 + m->right + 1) * m->unit + 16) / kPage + 2;
-    if (sinks + run < pages) pages = sinks + run;
-  }
-  if (pages < 1) pages = 1;
-  const long long all = pages * B * Hkv * p.row_tiles;
-  long long per = (all / 1024 + 3) / 4 * 4;
-  per = per < 4 ? 4 : per > 32 ? 32 : per;
-  p.per_part = (int)per;
-  p.parts = (int)((pages + per - 1) / per);
+  const long long groups = (long long)B * Hkv * (((long long)max_q * G + 15) / 16);
+  TokenPlan p;
+  // one generation (two workgroups a compute unit) where that is enough for all, else several
+  p.target = (int)(groups <= 256 ? 512 - groups : 4 * groups);
+  p.groups = (int)groups;
+  p.one = max_pages <= 4;
+  p.grid = p.one ? p.groups : p.target + p.groups;
   return p;
 }
 size_t cache_parts(int B, int H, int Hkv, int d, int max_q, int max_pages) {
-  const TokenPlan p = token_plan(B, H, Hkv, max_q, max_pages, nullptr);
-  return (size_t)B * Hkv * p.row_tiles * p.parts * 16 * (d + 2);
+  const TokenPlan p = token_plan(B, H, Hkv, max_q, max_pages);
+  return p.one ? 0 : (size_t)p.grid * 16 * (d + 2);
+}
+// Which sequence a workgroup works for, and what of it.
+struct TokenItem {
+  int b, hk, rt, part, parts, per;  // its part of `parts`, of `per` pages
+  int first;                        // slot of part 0 of its (sequence, key head, row tile); further parts: `step` slots on
+  int step;
+};
+__device__ __forceinline__ int token_pages(const WinArgs& a, const CacheArgs& c, int b, int nq) {
+  if (nq == 0) return 0;
+  const int nk = max(0, min(c.lens[b], c.max_pages * kPage));
+  return max(1, WinWalk(a.mask, nk - nq, nk - 1, nk, kPage, kPage).n);
+}
+// Item number `item` of all, or, JOIN, its number among the items that are the first of their triple; false: there are fewer.  (All
+// lanes of a wavefront.)
+template <bool JOIN>
+__device__ __forceinline__ bool token_item(const WinArgs& a, const CacheArgs& c, const TokenPlan& plan, unsigned item, TokenItem& t) {
+  const int lane = threadIdx.x & 63;
+  auto of = [&](int b, int& pages, int& groups) {  // of sequence b: pages, (key head, row tile) pairs
+    const int nq = b < a.B ? win_seq(a.rq, b).n : 0;
+    groups = a.Hkv * ((nq * a.G + 15) / 16);
+    pages = b < a.B ? token_pages(a, c, b, nq) : 0;
+  };
+  auto sum = [](long long x) {
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m);
+    return x;
+  };
+  int pages, groups;
+  of(lane, pages, groups);
+  long long total = (long long)pages * groups;
+  for (int b = 64 + lane; b - lane < a.B; b += 64) {
+    int p, g;
+    of(b, p, g);
+    total += (long long)p * g;
+  }
+  total = sum(total);
+  t.per = plan.one ? 4 : (int)max(4ll, (total / plan.target + 4) / 4 * 4);
+  unsigned before = 0, slots = 0;  // items and slots of the sequences ahead
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    if (b0) of(b0 + lane, pages, groups);
+    const int parts = (pages + t.per - 1) / t.per;
+    const unsigned places = (unsigned)(parts * groups), mine = JOIN ? (unsigned)groups : places;
+    auto running = [&](unsigned x) {
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) {
+        const unsigned y = __shfl_up(x, m);
+        if (lane >= m) x += y;
+      }
+      return x;
+    };
+    const unsigned upto = running(mine), slots_upto = JOIN ? running(places) : upto;
+    const unsigned long long past = __ballot(before + upto > item);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      t.b = b0 + l;
+      const unsigned at = before + (unsigned)__builtin_amdgcn_readlane((int)(upto - mine), l);
+      const int g = __builtin_amdgcn_readlane(groups, l), k = (int)(item - at);
+      t.parts = __builtin_amdgcn_readlane(parts, l);
+      t.part = k / g;
+      const int r = k - t.part * g, tiles = g / a.Hkv;
+      t.hk = r / tiles;
+      t.rt = r - t.hk * tiles;
+      t.first = (int)(slots + (unsigned)__builtin_amdgcn_readlane((int)(slots_upto - places), l)) + r;
+      t.step = g;
+      t.b = __builtin_amdgcn_readfirstlane(t.b);
+      t.per = __builtin_amdgcn_readfirstlane(t.per);
+      t.part = __builtin_amdgcn_readfirstlane(t.part);
+      t.hk = __builtin_amdgcn_readfirstlane(t.hk);
+      t.rt = __builtin_amdgcn_readfirstlane(t.rt);
+      return true;
+    }
+    before += (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
+    slots += (unsigned)__builtin_amdgcn_readlane((int)slots_upto, 63);
+  }
+  return false;
 }
 
 template <int D, bool F16>
@@ -192,32 +278,44 @@ __global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cac
   constexpr int KL = D / 64, VT = D / 16;  // 16-byte loads a row of K, tiles of 16 dv
   __shared__ float lds_o[4][16 * D];
   __shared__ float lds_ml[4][16][2];
-  const int part = blockIdx.x % plan.parts, rest = blockIdx.x / plan.parts;
-  const int rt = rest % plan.row_tiles, bh = rest / plan.row_tiles, hk = bh % a.Hkv, b = bh / a.Hkv;
+  TokenItem at;
+  if (!token_item<false>(a, cache, plan, blockIdx.x, at)) return;
+  const int rt = at.rt, hk = at.hk, b = at.b;
   const WinSeq sq = win_seq(a.rq, b);
   const int rows = min(16, sq.n * a.G - rt * 16);
-  if (rows <= 0) return;
-  const int nk = max(0, min(cache.lens[b], cache.max_pages * kPage)), shift = nk - sq.n;
-  const WinWalk walk(a.mask, rt * 16 / a.G + shift, (rt * 16 + rows - 1) / a.G + shift, nk, kPage, kPage);
-  const int p0 = part * plan.per_part, p1 = min(walk.n, p0 + plan.per_part);
-  if (p0 >= walk.n && part > 0) return;
+  const int nk = __builtin_amdgcn_readfirstlane(max(0, min(cache.lens[b], cache.max_pages * kPage))), shift = nk - sq.n;
+  WinWalk walk(a.mask, rt * 16 / a.G + shift, (rt * 16 + rows - 1) / a.G + shift, nk, kPage, kPage);
+  walk.uniform();
+  // (a tile may walk fewer pages than the sequence: parts behind them are empty)
+  const int p0 = min(walk.n, at.part * at.per), p1 = min(walk.n, p0 + at.per);
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, g = lane >> 4;
   const int row = rt * 16 + min(m, rows - 1), qi = row / a.G, hq = hk * a.G + row % a.G;
   const WinSpan span = win_span(a.mask, qi + shift, nk);
-  // the wavefront's pages, one a lane
+  // the wavefront's pages, 64 at a time, one a lane
   const int np = p1 - p0 > wave ? (p1 - p0 - wave + 3) / 4 : 0;
-  int id = -1;
+  int id = -1, chunk = -1;
   float sks = 1.f, svs = 1.f;
-  if (lane < np) {
-    id = cache.table[(long long)b * cache.max_pages + walk.begin(p0 + wave + 4 * lane) / kPage];
-    if ((unsigned)id >= (unsigned)cache.pages) id = -1;
-    if (id >= 0) {
-      sks = cache.ks[(long long)id * a.Hkv + hk];
-      svs = cache.vs[(long long)id * a.Hkv + hk];
+  auto want = [&](int i) {
+    if (i >> 6 == chunk) return;
+    chunk = i >> 6;
+    const int mine = chunk * 64 + lane;
+    id = -1, sks = 1.f, svs = 1.f;
+    if (mine < np) {
+      id = cache.table[(long long)b * cache.max_pages + walk.begin(p0 + wave + 4 * mine) / kPage];
+      if ((unsigned)id >= (unsigned)cache.pages) id = -1;
+      if (id >= 0) {
+        sks = cache.ks[(long long)id * a.Hkv + hk];
+        svs = cache.vs[(long long)id * a.Hkv + hk];
+      }
     }
-  }
+  };
+  // of page i
+  struct Scales {
+    float f, lv;
+    bool there;
+  };
   bf16x8 qreg[2 * KL];
   {
     const uint4* p = (const uint4*)a.q.row(b, sq.row0 + qi, hq);
@@ -232,10 +330,14 @@ __global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cac
   struct Page {
     uint4 k[4][KL], v[VT];
   };
-  auto fetch = [&](int i, Page& p) {
-    const int at = max(__builtin_amdgcn_readlane(id, min(i, max(np - 1, 0)) & 63), 0);
-    const uint8_t* kp = cache.k + ((long long)at * a.Hkv + hk) * (kPage * D);
-    const uint8_t* vp = cache.v + ((long long)at * a.Hkv + hk) * (kPage * D);
+  auto fetch = [&](int i, Page& p, Scales& sc) {
+    want(i);
+    sc.there = __builtin_amdgcn_readlane(id, i & 63) >= 0;
+    sc.f = sl2 * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sks), i & 63));
+    sc.lv = fast_log2(__int_as_float(__builtin_amdgcn_readlane(__float_as_int(svs), i & 63)));
+    const int page = max(__builtin_amdgcn_readlane(id, i & 63), 0);
+    const uint8_t* kp = cache.k + ((long long)page * a.Hkv + hk) * (kPage * D);
+    const uint8_t* vp = cache.v + ((long long)page * a.Hkv + hk) * (kPage * D);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -243,11 +345,10 @@ __global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cac
 #pragma unroll
     for (int x = 0; x < VT; ++x) p.v[x] = *(const uint4*)(vp + (16 * x + m) * kPage + 16 * g);
   };
-  auto multiply = [&](int i, Page& p) {
+  auto multiply = [&](int i, Page& p, const Scales& sc) {
     const int piece = p0 + wave + 4 * i, key0 = walk.begin(piece);
-    if (__builtin_amdgcn_readlane(id, i & 63) < 0) return;  // (names no page: hidden)
-    const float f = sl2 * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sks), i & 63));
-    const float lv = fast_log2(__int_as_float(__builtin_amdgcn_readlane(__float_as_int(svs), i & 63)));
+    if (!sc.there) return;  // (the entry names no page: hidden)
+    const float f = sc.f, lv = sc.lv;
     f32x4 s[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -315,14 +416,21 @@ __global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cac
   };
   if (np > 0) {
     Page pa, pb;
-    fetch(0, pa);
-    for (int i = 0; i < np; i += 2) {
-      fetch(i + 1, pb);
-      multiply(i, pa);
-      if (i + 1 < np) {
-        fetch(i + 2, pa);
-        multiply(i + 1, pb);
-      }
+    Scales sa, sb;
+    fetch(0, pa, sa);
+    int i = 0;
+    for (; i + 2 < np; i += 2) {
+      fetch(i + 1, pb, sb);
+      multiply(i, pa, sa);
+      fetch(i + 2, pa, sa);
+      multiply(i + 1, pb, sb);
+    }
+    if (i + 1 < np) {
+      fetch(i + 1, pb, sb);
+      multiply(i, pa, sa);
+      multiply(i + 1, pb, sb);
+    } else {
+      multiply(i, pa, sa);
     }
   }
   sum += __shfl_xor(sum, 16);
@@ -345,8 +453,8 @@ __global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cac
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] += f * y0[e], v[4 + e] += f * y1[e];
     }
-    const int at = rt * 16 + r, q_of = at / a.G, h_of = hk * a.G + at % a.G;
-    if (plan.parts == 1) {
+    const int row_of = rt * 16 + r, q_of = row_of / a.G, h_of = hk * a.G + row_of % a.G;
+    if (at.parts == 1) {
       const bool none = M <= kNoRow;
       const float inv = none ? 0.f : 1.f / L;
       const uint4 u = {pack16<F16>(v[0] * inv, v[1] * inv), pack16<F16>(v[2] * inv, v[3] * inv), pack16<F16>(v[4] * inv, v[5] * inv),
@@ -354,7 +462,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cac
       *((uint4*)a.o.out(b, sq.row0 + q_of, h_of) + ch) = u;
       if (a.lse && ch == 0) a.lse[a.stat(h_of, b, sq.row0, q_of)] = none ? -INFINITY : (M + fast_log2(L)) * kLn2;
     } else {
-      float* const to = parts + (((long long)bh * plan.row_tiles + rt) * plan.parts + part) * (16 * (D + 2));
+      float* const to = parts + (long long)blockIdx.x * (16 * (D + 2));
       *(float4*)&to[r * D + ch * 8] = make_float4(v[0], v[1], v[2], v[3]);
       *(float4*)&to[r * D + ch * 8 + 4] = make_float4(v[4], v[5], v[6], v[7]);
       if (ch == 0) *(float2*)&to[16 * D + 2 * r] = make_float2(M, L);
@@ -367,18 +475,18 @@ template <int D, bool F16>
 __global__ __launch_bounds__(256) void k_cache_join(WinArgs a, CacheArgs cache, const float* __restrict__ parts, TokenPlan plan) {
   constexpr int CH = D / 8, PG = 256 / CH;
   __shared__ float so[PG][D + 4], sm[PG], sl[PG];
-  const int r = blockIdx.x % 16, rest = blockIdx.x / 16, rt = rest % plan.row_tiles, bh = rest / plan.row_tiles, hk = bh % a.Hkv, b = bh / a.Hkv;
+  TokenItem at;
+  const int r = blockIdx.x % 16;
+  if (!token_item<true>(a, cache, plan, blockIdx.x / 16, at) || at.parts == 1) return;
+  const int rt = at.rt, hk = at.hk, b = at.b;
   const WinSeq sq = win_seq(a.rq, b);
-  const int rows = min(16, sq.n * a.G - rt * 16);
-  if (r >= rows) return;
-  const int nk = max(0, min(cache.lens[b], cache.max_pages * kPage)), shift = nk - sq.n;
-  const WinWalk walk(a.mask, rt * 16 / a.G + shift, (rt * 16 + rows - 1) / a.G + shift, nk, kPage, kPage);
-  const int live = max(1, (walk.n + plan.per_part - 1) / plan.per_part);
-  const int tid = threadIdx.x, ch = tid % CH, pg = tid / CH;
-  const float* from = parts + ((long long)bh * plan.row_tiles + rt) * plan.parts * (16 * (D + 2));
+  if (r >= min(16, sq.n * a.G - rt * 16)) return;
+  const int tid = threadIdx.x, ch = tid % CH, pg = tid / CH, live = at.parts;
+  const float* from = parts + (long long)at.first * (16 * (D + 2));
+  const long long step = (long long)at.step * (16 * (D + 2));
   float M = kNoRow, L = 0.f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   for (int p = pg; p < live; p += PG) {
-    const float* x = from + (long long)p * (16 * (D + 2));
+    const float* x = from + p * step;
     const float2 ml = *(const float2*)&x[16 * D + 2 * r];
     const float4 y0 = *(const float4*)&x[r * D + ch * 8], y1 = *(const float4*)&x[r * D + ch * 8 + 4];
     const float mn = fmaxf(M, ml.x), fa = fast_exp2(M - mn), fb = fast_exp2(ml.x - mn);
@@ -407,7 +515,7 @@ __global__ __launch_bounds__(256) void k_cache_join(WinArgs a, CacheArgs cache, 
   }
   const bool none = M <= kNoRow;
   const float inv = none ? 0.f : 1.f / L;
-  const int at = rt * 16 + r, q_of = at / a.G, h_of = hk * a.G + at % a.G;
+  const int row_of = rt * 16 + r, q_of = row_of / a.G, h_of = hk * a.G + row_of % a.G;
   const uint4 u = {pack16<F16>(v[0] * inv, v[1] * inv), pack16<F16>(v[2] * inv, v[3] * inv), pack16<F16>(v[4] * inv, v[5] * inv),
                    pack16<F16>(v[6] * inv, v[7] * inv)};
   *((uint4*)a.o.out(b, sq.row0 + q_of, h_of) + tid) = u;
@@ -417,14 +525,11 @@ __global__ __launch_bounds__(256) void k_cache_join(WinArgs a, CacheArgs cache, 
 namespace {
 template <int D, bool F16>
 hipError_t token(const WinArgs& a, const CacheArgs& c, float* parts, hipStream_t s) {
-  const TokenPlan full = token_plan(a.B, a.H, a.Hkv, a.rq.most, c.max_pages, nullptr);
-  TokenPlan plan = token_plan(a.B, a.H, a.Hkv, a.rq.most, c.max_pages, &a.mask);
-  if (plan.parts > full.parts) plan = full;  // (the workspace is sized without the mask)
-  const unsigned tiles = (unsigned)a.B * a.Hkv * plan.row_tiles;
-  k_cache_token<D, F16><<<tiles * plan.parts, 256, 0, s>>>(a, c, parts, plan);
+  const TokenPlan plan = token_plan(a.B, a.H, a.Hkv, a.rq.most, c.max_pages);
+  k_cache_token<D, F16><<<(unsigned)plan.grid, 256, 0, s>>>(a, c, parts, plan);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || plan.parts == 1) return e;
-  k_cache_join<D, F16><<<tiles * 16, 256, 0, s>>>(a, c, parts, plan);
+  if (e != hipSuccess || plan.one) return e;
+  k_cache_join<D, F16><<<(unsigned)plan.groups * 16u, 256, 0, s>>>(a, c, parts, plan);
   return hipGetLastError();
 }
 }  // namespace

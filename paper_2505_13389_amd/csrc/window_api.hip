@@ -105,6 +105,9 @@ struct Recorded {
     if ((expr) != hipSuccess) return VSA_ERR_HIP; \
   } while (0)
 
+// Few rows a key head (the heads of its group times the queries): the pages are split over workgroups.
+bool few_rows(const vsa_cache_t* p) { return (long long)p->max_q * (p->H / p->Hkv) <= 128; }
+
 int check_cache(const vsa_cache_t* p, bool attention) {
   if (!p) return VSA_ERR_NULL;
   const int rc = attention ? check_common(p->B, p->H, p->Hkv, p->d, p->unit, p->left, p->right, p->sinks, p->softmax_scale, p->dtype)
@@ -115,11 +118,9 @@ int check_cache(const vsa_cache_t* p, bool attention) {
     return VSA_ERR_UNSUPPORTED;
   const long long heads = attention ? p->H : p->Hkv;
   if (blocks_of(p->B, ((long long)p->max_q / 64 + 2) * heads) > kMostBlocks) return VSA_ERR_UNSUPPORTED;
+  if (attention && few_rows(p) && (long long)p->B * p->Hkv * 8 > kMostBlocks / 16) return VSA_ERR_UNSUPPORTED;  // (row tiles are 8 at most)
   return VSA_OK;
 }
-
-// Few rows a key head (the heads of its group times the queries): the pages are split over workgroups.
-bool few_rows(const vsa_cache_t* p) { return (long long)p->max_q * (p->H / p->Hkv) <= 128; }
 
 size_t cache_bytes(const vsa_cache_t* p) {
   return (few_rows(p) ? vsa::cache_parts(p->B, p->H, p->Hkv, p->d, p->max_q, p->max_pages) * sizeof(float) : 0) + 16;
