@@ -247,12 +247,12 @@ typedef struct {
 /* Attention of q [.., H, d] over k, v [.., Hkv, d]:  out = softmax(scale q k^T over the visible keys) v.
  *   cu_q, cu_k   in  int32 [B+1], both (packed) or neither (dense)
  *   lse          out fp32 [H, rows], rows = total_q (packed) or B*max_q (dense): log-sum-exp of the scaled logits, or NULL */
+size_t vsa_window_workspace_bytes(const vsa_window_t* p, int backward); /* 0 for invalid parameters.  Host-only. */
 int vsa_window_forward(const vsa_window_t* p, const void* q, const void* k, const void* v, const int32_t* cu_q,
-                       const int32_t* cu_k, void* out, float* lse, void* hip_stream);
+                       const int32_t* cu_k, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Its gradients.  out and lse as the forward wrote them; dq, dk, dv are written whole (keys that no query sees: zeros), the heads
  * of a group summed into their key head in fp32.  fp16: dS = P (dP - rowsum(dout out)) must stay below 65504. */
-size_t vsa_window_workspace_bytes(const vsa_window_t* p); /* of the backward; 0 for invalid parameters.  Host-only. */
 int vsa_window_backward(const vsa_window_t* p, const void* q, const void* k, const void* v, const int32_t* cu_q,
                         const int32_t* cu_k, const void* out, const void* dout, const float* lse, void* dq, void* dk, void* dv,
                         void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -92,8 +92,7 @@ class _WindowAttention(torch.autograd.Function):
         dout = _rows_of_16_bytes(dout)
         new = torch.empty if cu_q is None else torch.zeros
         dq, dk, dv = (new(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
-        workspace = torch.empty(window.vsa_window_workspace_bytes(ctx.pb), dtype=torch.uint8, device=q.device)
-        window.vsa_window_backward(ctx.pb, q, k, v, out, dout, lse, dq, dk, dv, workspace, cu_q, cu_k)
+        window.vsa_window_backward(ctx.pb, q, k, v, out, dout, lse, dq, dk, dv, None, cu_q, cu_k)
         return dq, dk, dv, None, None, None
 
 

@@ -32,7 +32,7 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ float finite_or_nan(float x) { return x - x == 0.f ? x : __uint_as_float(0x7fc00000u); }
 
 // LARGE: every XCD takes a contiguous run of the launch (pages and heads whose rows lie side by side), and what is written goes past the
-// caches: 75600 tokens, 40 heads, d = 128 454 -> LARGE_US us.
+// caches: 75600 tokens, 40 heads, d = 128 454 -> 412 us.
 template <int D, bool F16, bool LARGE>
 __global__ __launch_bounds__(2 * D) void k_cache_append(AppendArgs a, int most_pages) {
   constexpr int CPR = D / 8, NT = 2 * D, NWV = NT / 64;
@@ -179,6 +179,7 @@ constexpr float kNoRow = -1e30f;
 // wavefronts) and the same for all sequences; a sequence has as many parts as it needs.  Then all workgroups run side by side, take
 // about as long as each other, and none is launched for pages that are not there.
 struct TokenPlan {
+  int tiles;                 // row tiles of the longest sequence
   int target, groups, grid;  // workgroups aimed at; (sequence, key head, row tile) triples; workgroups needed at most
   int one;           // every sequence has one part, whatever its length: nothing is joined
 };
@@ -188,6 +189,7 @@ static TokenPlan token_plan(int B, int H, int Hkv, int max_q, int max_pages) {
   TokenPlan p;
   // one generation (two workgroups a compute unit) where that is enough for all, else several
   p.target = (int)(groups <= 256 ? 512 - groups : 4 * groups);
+  p.tiles = (int)(((long long)max_q * G + 15) / 16);
   p.groups = (int)groups;
   p.one = max_pages <= 4;
   p.grid = p.one ? p.groups : p.target + p.groups;
@@ -195,7 +197,7 @@ static TokenPlan token_plan(int B, int H, int Hkv, int max_q, int max_pages) {
 }
 size_t cache_parts(int B, int H, int Hkv, int d, int max_q, int max_pages) {
   const TokenPlan p = token_plan(B, H, Hkv, max_q, max_pages);
-  return p.one ? 0 : (size_t)p.grid * 16 * (d + 2);
+  return p.one ? 0 : (size_t)p.grid * 16 * (d + 2) + (size_t)p.groups * 4;
 }
 // Which sequence a workgroup works for, and what of it.
 struct TokenItem {
@@ -208,9 +210,7 @@ __device__ __forceinline__ int token_pages(const WinArgs& a, const CacheArgs& c,
   const int nk = max(0, min(c.lens[b], c.max_pages * kPage));
   return max(1, WinWalk(a.mask, nk - nq, nk - 1, nk, kPage, kPage).n);
 }
-// Item number `item` of all, or, JOIN, its number among the items that are the first of their triple; false: there are fewer.  (All
-// lanes of a wavefront.)
-template <bool JOIN>
+// item number `item` of all; false: there are fewer.  (All lanes of a wavefront.)
 __device__ __forceinline__ bool token_item(const WinArgs& a, const CacheArgs& c, const TokenPlan& plan, unsigned item, TokenItem& t) {
   const int lane = threadIdx.x & 63;
   auto of = [&](int b, int& pages, int& groups) {  // of sequence b: pages, (key head, row tile) pairs
@@ -233,20 +233,17 @@ __device__ __forceinline__ bool token_item(const WinArgs& a, const CacheArgs& c,
   }
   total = sum(total);
   t.per = plan.one ? 4 : (int)max(4ll, (total / plan.target + 4) / 4 * 4);
-  unsigned before = 0, slots = 0;  // items and slots of the sequences ahead
+  unsigned before = 0;  // items of the sequences ahead
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     if (b0) of(b0 + lane, pages, groups);
     const int parts = (pages + t.per - 1) / t.per;
-    const unsigned places = (unsigned)(parts * groups), mine = JOIN ? (unsigned)groups : places;
-    auto running = [&](unsigned x) {
+    const unsigned mine = (unsigned)(parts * groups);
+    unsigned upto = mine;
 #pragma unroll
-      for (int m = 1; m < 64; m <<= 1) {
-        const unsigned y = __shfl_up(x, m);
-        if (lane >= m) x += y;
-      }
-      return x;
-    };
-    const unsigned upto = running(mine), slots_upto = JOIN ? running(places) : upto;
+    for (int m = 1; m < 64; m <<= 1) {
+      const unsigned x = __shfl_up(upto, m);
+      if (lane >= m) upto += x;
+    }
     const unsigned long long past = __ballot(before + upto > item);
     if (past) {
       const int l = __builtin_ctzll(past);
@@ -258,7 +255,7 @@ __device__ __forceinline__ bool token_item(const WinArgs& a, const CacheArgs& c,
       const int r = k - t.part * g, tiles = g / a.Hkv;
       t.hk = r / tiles;
       t.rt = r - t.hk * tiles;
-      t.first = (int)(slots + (unsigned)__builtin_amdgcn_readlane((int)(slots_upto - places), l)) + r;
+      t.first = (int)at + r;
       t.step = g;
       t.b = __builtin_amdgcn_readfirstlane(t.b);
       t.per = __builtin_amdgcn_readfirstlane(t.per);
@@ -268,7 +265,6 @@ __device__ __forceinline__ bool token_item(const WinArgs& a, const CacheArgs& c,
       return true;
     }
     before += (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
-    slots += (unsigned)__builtin_amdgcn_readlane((int)slots_upto, 63);
   }
   return false;
 }
@@ -279,7 +275,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cac
   __shared__ float lds_o[4][16 * D];
   __shared__ float lds_ml[4][16][2];
   TokenItem at;
-  if (!token_item<false>(a, cache, plan, blockIdx.x, at)) return;
+  if (!token_item(a, cache, plan, blockIdx.x, at)) return;
   const int rt = at.rt, hk = at.hk, b = at.b;
   const WinSeq sq = win_seq(a.rq, b);
   const int rows = min(16, sq.n * a.G - rt * 16);
@@ -439,6 +435,8 @@ __global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cac
 #pragma unroll
   for (int x = 0; x < VT; ++x) *(f32x4*)&lds_o[wave][m * D + (((4 * x + g) ^ m) << 2)] = o[x];
   __syncthreads();
+  if (tid == 0 && at.part == 0 && !plan.one)  // for the join: where the parts are
+    ((int4*)(parts + (long long)plan.grid * (16 * (D + 2))))[(b * a.Hkv + hk) * plan.tiles + rt] = make_int4(at.first, at.parts, at.step, 0);
   // rows of the tile, 8 elements a thread
   for (int it = tid; it < rows * (D / 8); it += 256) {
     const int r = it / (D / 8), ch = it % (D / 8);
@@ -475,15 +473,14 @@ template <int D, bool F16>
 __global__ __launch_bounds__(256) void k_cache_join(WinArgs a, CacheArgs cache, const float* __restrict__ parts, TokenPlan plan) {
   constexpr int CH = D / 8, PG = 256 / CH;
   __shared__ float so[PG][D + 4], sm[PG], sl[PG];
-  TokenItem at;
-  const int r = blockIdx.x % 16;
-  if (!token_item<true>(a, cache, plan, blockIdx.x / 16, at) || at.parts == 1) return;
-  const int rt = at.rt, hk = at.hk, b = at.b;
+  const int r = blockIdx.x % 16, group = blockIdx.x / 16, rt = group % plan.tiles, hk = group / plan.tiles % a.Hkv, b = group / plan.tiles / a.Hkv;
   const WinSeq sq = win_seq(a.rq, b);
   if (r >= min(16, sq.n * a.G - rt * 16)) return;
-  const int tid = threadIdx.x, ch = tid % CH, pg = tid / CH, live = at.parts;
-  const float* from = parts + (long long)at.first * (16 * (D + 2));
-  const long long step = (long long)at.step * (16 * (D + 2));
+  const int4 at = ((const int4*)(parts + (long long)plan.grid * (16 * (D + 2))))[group];  // first slot, parts, slots from one to the next
+  const int tid = threadIdx.x, ch = tid % CH, pg = tid / CH, live = at.y;
+  if (live == 1) return;
+  const float* from = parts + (long long)at.x * (16 * (D + 2));
+  const long long step = (long long)at.z * (16 * (D + 2));
   float M = kNoRow, L = 0.f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   for (int p = pg; p < live; p += PG) {
     const float* x = from + p * step;

@@ -77,6 +77,7 @@ WinArgs window_args(const vsa_window_t* p, bool packed, const int32_t* cu_q, con
 
 // of the backward: the rows' terms, then partial results
 size_t terms_bytes(const WinArgs& a) { return ((size_t)a.H * a.lse_rows * 8 + 255) / 256 * 256; }
+size_t fwd_bytes(const vsa_window_t* p, const WinArgs& a) { return vsa::row_parts(a, p->max_k, p->d) * sizeof(float) + 16; }
 size_t bwd_bytes(const vsa_window_t* p, const WinArgs& a) { return terms_bytes(a) + vsa::window_parts(a, p->d) * sizeof(float) + 16; }
 
 int check_window_strides(const vsa_window_t* p, bool packed, bool backward) {
@@ -122,8 +123,19 @@ int check_cache(const vsa_cache_t* p, bool attention) {
   return VSA_OK;
 }
 
-size_t cache_bytes(const vsa_cache_t* p) {
-  return (few_rows(p) ? vsa::cache_parts(p->B, p->H, p->Hkv, p->d, p->max_q, p->max_pages) * sizeof(float) : 0) + 16;
+WinArgs cache_args(const vsa_cache_t* p, const int32_t* cu) {
+  WinArgs a = {};
+  a.mask = {p->unit, p->left, p->right, p->sinks};
+  a.B = p->B, a.H = p->H, a.Hkv = p->Hkv, a.G = p->H / p->Hkv;
+  a.rq = {cu, p->max_q, cu ? p->total_q : (long long)p->max_q};
+  a.lse_rows = cu ? p->total_q : (long long)p->B * p->max_q;
+  a.scale = scale_or_default(p->softmax_scale, p->d);
+  return a;
+}
+size_t cache_bytes(const vsa_cache_t* p, const WinArgs& a) {
+  const size_t floats = few_rows(p) ? vsa::cache_parts(p->B, p->H, p->Hkv, p->d, p->max_q, p->max_pages)
+                                    : vsa::row_parts(a, (long long)p->max_pages * vsa::kPage, p->d);
+  return floats * sizeof(float) + 16;
 }
 
 // every visible pair once, no other unmasked: blocks of queries over keys, in pieces
@@ -192,28 +204,36 @@ int64_t replay_keys(const vsa::WinMask& m, int nq, int nk, int block) {
 extern "C" {
 
 int vsa_window_forward(const vsa_window_t* p, const void* q, const void* k, const void* v, const int32_t* cu_q,
-                       const int32_t* cu_k, void* out, float* lse, void* hip_stream) {
+                       const int32_t* cu_k, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
   int rc = check_window(p);
   if (rc != VSA_OK) return rc;
   if (!cu_q != !cu_k) return VSA_ERR_BAD_ARG;
   const bool packed = cu_q != nullptr;
   const long long rows = stat_rows(p, packed), keys = packed ? p->total_k : (long long)p->B * p->max_k;
   if ((rows && (!q || !out)) || (keys && (!k || !v))) return VSA_ERR_NULL;
-  if (off(q, 16) || off(k, 16) || off(v, 16) || off(out, 16) || off(lse, 4) || off(cu_q, 4) || off(cu_k, 4)) return VSA_ERR_ALIGN;
+  if (off(q, 16) || off(k, 16) || off(v, 16) || off(out, 16) || off(lse, 4) || off(cu_q, 4) || off(cu_k, 4) || off(workspace, 16))
+    return VSA_ERR_ALIGN;
   if ((rc = check_window_strides(p, packed, false)) != VSA_OK) return rc;
-  if (rows == 0 || p->max_q == 0) return VSA_OK;
   WinArgs a = window_args(p, packed, cu_q, cu_k);
+  if (!workspace || workspace_bytes < fwd_bytes(p, a)) return VSA_ERR_WORKSPACE;
+  if (rows == 0 || p->max_q == 0) return VSA_OK;
   a.q = view(q, p->q, packed), a.k = view(k, p->k, packed), a.v = view(v, p->v, packed), a.o = view(out, p->out, packed);
   a.lse = lse;
   hipStream_t s = (hipStream_t)hip_stream;
-  VSA_LAUNCH("window_fwd", vsa::launch_window_fwd(a, p->d, p->dtype == VSA_DTYPE_FP16, s));
+  VSA_LAUNCH("window_fwd", vsa::launch_window_fwd(a, p->d, p->dtype == VSA_DTYPE_FP16, (float*)workspace, s));
   return VSA_OK;
 }
 
-size_t vsa_window_workspace_bytes(const vsa_window_t* p) {
+size_t vsa_window_workspace_bytes(const vsa_window_t* p, int backward) {
   if (check_window(p) != VSA_OK) return 0;
-  const size_t dense = bwd_bytes(p, window_args(p, false, nullptr, nullptr)), packed = bwd_bytes(p, window_args(p, true, nullptr, nullptr));
-  return dense > packed ? dense : packed;
+  size_t most = 0;
+  for (int packed = 0; packed < 2; ++packed) {  // (which of them it is the call says)
+    const int32_t* const cu = packed ? (const int32_t*)p : nullptr;  // (never read: not null is all that counts here)
+    const WinArgs a = window_args(p, packed != 0, cu, cu);
+    const size_t bytes = backward ? bwd_bytes(p, a) : fwd_bytes(p, a);
+    most = bytes > most ? bytes : most;
+  }
+  return most;
 }
 
 int vsa_window_backward(const vsa_window_t* p, const void* q, const void* k, const void* v, const int32_t* cu_q,
@@ -264,7 +284,11 @@ int vsa_cache_append(const vsa_cache_t* p, const void* k, const void* v, const i
   return VSA_OK;
 }
 
-size_t vsa_cache_workspace_bytes(const vsa_cache_t* p) { return check_cache(p, true) == VSA_OK ? cache_bytes(p) : 0; }
+size_t vsa_cache_workspace_bytes(const vsa_cache_t* p) {
+  if (check_cache(p, true) != VSA_OK) return 0;
+  const size_t dense = cache_bytes(p, cache_args(p, nullptr)), packed = cache_bytes(p, cache_args(p, (const int32_t*)p));  // (not read)
+  return dense > packed ? dense : packed;
+}
 
 int vsa_cache_attention(const vsa_cache_t* p, const void* q, const int32_t* cu, const int32_t* lens, const int32_t* table,
                         const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale, void* out, float* lse,
@@ -279,14 +303,9 @@ int vsa_cache_attention(const vsa_cache_t* p, const void* q, const int32_t* cu, 
     return VSA_ERR_ALIGN;
   const long long nb = packed ? 1 : p->B, n = packed ? p->total_q : p->max_q;
   if ((rc = check_strides(p->q, nb, n, p->H, 0)) != VSA_OK || (rc = check_strides(p->out, nb, n, p->H, p->d)) != VSA_OK) return rc;
-  if (!workspace || workspace_bytes < cache_bytes(p)) return VSA_ERR_WORKSPACE;
+  WinArgs a = cache_args(p, cu);
+  if (!workspace || workspace_bytes < cache_bytes(p, a)) return VSA_ERR_WORKSPACE;
   if (rows == 0 || p->max_q == 0) return VSA_OK;
-  WinArgs a = {};
-  a.mask = {p->unit, p->left, p->right, p->sinks};
-  a.B = p->B, a.H = p->H, a.Hkv = p->Hkv, a.G = p->H / p->Hkv;
-  a.rq = {cu, p->max_q, packed ? p->total_q : (long long)p->max_q};
-  a.lse_rows = rows;
-  a.scale = scale_or_default(p->softmax_scale, p->d);
   a.q = view(q, p->q, packed), a.o = view(out, p->out, packed);
   a.lse = lse;
   const vsa::CacheArgs c = {(uint8_t*)const_cast<void*>(k_pages), (uint8_t*)const_cast<void*>(v_pages), const_cast<float*>(k_scale),
@@ -294,7 +313,7 @@ int vsa_cache_attention(const vsa_cache_t* p, const void* q, const int32_t* cu, 
   hipStream_t s = (hipStream_t)hip_stream;
   const bool f16 = p->dtype == VSA_DTYPE_FP16;
   if (few_rows(p)) VSA_LAUNCH("cache_token", vsa::launch_cache_token(a, c, p->d, f16, (float*)workspace, s));
-  else VSA_LAUNCH("cache_chunk", vsa::launch_cache_chunk(a, c, p->d, f16, s));
+  else VSA_LAUNCH("cache_chunk", vsa::launch_cache_chunk(a, c, p->d, f16, (float*)workspace, s));
   return VSA_OK;
 }
 

@@ -159,15 +159,15 @@ __device__ __forceinline__ void store_part(f32x16 (&acc)[D / 32][2], float* buf,
 //   dQ += K^T dS(u)    the first of P(u + 1), copies of V(u + 2)
 // K has three stages (of unit u to its end, of u + 1, of u + 2), V two.
 template <int D, bool F16, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, int nqb) {
+__global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan plan) {
   using TL = Tile<D>;
   constexpr int KS = D / 16, DVB = D / 32, HALF = 32 * D * 2, NC = RowCopy<D>::NC, PH = 2 * KS, IPM = 16 / PH;  // softmax items a matrix instruction
   constexpr int kAhead = 2, kEvery = PH / NC, kEarly = 4;  // kEarly: items of P done in the phase before its own
   constexpr int STAGES = 5 * HALF, PLACE = STAGES > 64 * D * 4 ? STAGES : 64 * D * 4;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * PLACE];
-  int b, hk, item;
-  if (!win_item(blockIdx.x, (unsigned)a.Hkv, (unsigned)(nqb * a.G), b, hk, item)) return;
-  const int g = item % a.G, qb = nqb - 1 - item / a.G, hq = hk * a.G + g;  // (the last queries have most to walk: they come first)
+  RowItem at;
+  if (!win_rows(a, plan, blockIdx.x, at)) return;
+  const int b = at.b, hk = at.hk, qb = at.qb, hq = hk * a.G + at.g;
   const WinSeq sq = win_seq(a.rq, b), sk = win_seq(a.rk, b);
   const int r0 = qb * 64, rows = min(64, sq.n - r0);
   if (rows <= 0) return;
@@ -445,51 +445,77 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, int nqb) {
 // walked in parts of its own, which leave their sums in fp32 to be added, in order, by k_window_join.  Blocks of sinks, which every
 // later query sees, are the long ones.
 struct DkvPlan {
-  int nkb, sink_blocks, sink_parts, parts;  // 64-key blocks of a head, those that may hold sinks, parts of each, of the others
-  int per;
-  long long slots;  // partial results of a head
-  __host__ __device__ int items() const { return sink_blocks * sink_parts + (nkb - sink_blocks) * parts; }
-  // item of a head -> its block, part and how many there may be
-  __host__ __device__ void at(int item, int& block, int& part, int& of) const {
-    const int first = sink_blocks * sink_parts;
-    of = item < first ? sink_parts : parts;
-    block = item < first ? item / of : sink_blocks + (item - first) / of;
-    part = item < first ? item % of : (item - first) % of;
-  }
-  __host__ __device__ int slot(int block, int part) const {
-    return block < sink_blocks ? block * sink_parts + part : sink_blocks * sink_parts + (block - sink_blocks) * parts + part;
-  }
+  int heads, per_head;                      // (dense: sequences times heads; packed: heads); items of each
+  int sinks, sink_blocks, sink_parts;       // sequences of a head whose first blocks may hold sinks; those blocks, parts of each
+  int blocks, parts;                        // 64-key blocks of a head (of all sequences, at most); parts of each that holds no sink
+  int per, nw;
+  long long slots;                          // partial results of a head
+  // item of a head: those of the sinks come first.  Their slots are numbered like the items.
+  __host__ __device__ int sink_items() const { return sinks * sink_blocks * sink_parts; }
   // parts that a block of so many units has work for
   __host__ __device__ int live(int units, int of) const {
     const int want = (units + per - 1) / per;
     return want < 1 ? 1 : want < of ? want : of;
   }
 };
+struct DkvItem {
+  int b, hk, block, part, of;
+};
+// item number `item` of a head (first part of a block: `item` of the join) -> what it is; false: nothing
+__device__ __forceinline__ bool dkv_item(const WinArgs& a, const DkvPlan& plan, int head, int item, DkvItem& t) {
+  const bool packed = a.rk.cu != nullptr;
+  const int first = plan.sink_items();
+  t.hk = packed ? head : head % a.Hkv;
+  if (item < first) {
+    t.of = plan.sink_parts;
+    t.part = item % t.of;
+    const int k = item / t.of;
+    t.block = k % plan.sink_blocks;
+    t.b = packed ? k / plan.sink_blocks : head / a.Hkv;
+    return true;
+  }
+  t.of = plan.parts;
+  t.part = (item - first) % t.of;
+  const int k = (item - first) / t.of;
+  if (packed) {
+    if (!win_find(a.rk, a.B, (unsigned)k, t.b, t.block)) return false;
+  } else {
+    t.b = head / a.Hkv;
+    t.block = k;
+  }
+  return t.block >= plan.sink_blocks;
+}
 
 static DkvPlan dkv_plan(const WinArgs& a) {
   DkvPlan p = {};
-  p.nkb = (a.rk.most + 63) / 64;
   const WinMask& m = a.mask;
-  const long long most = (a.rq.most + 31) / 32 + 1, blocks = (long long)a.B * a.Hkv;
-  const long long ur_ = m.left < 0 || m.right < 0 ? most : ((long long)(m.left + m.right + 2) * m.unit + 64) / 32 + 2;
-  const long long ur = (ur_ < most ? ur_ : most) * a.G, us = most * a.G;
-  const long long sinks = ur_ < most ? (long long)m.sinks * m.unit : 0, sb = (sinks + 63) / 64;
-  p.sink_blocks = (int)(sb < p.nkb ? sb : p.nkb);
-  const long long total = blocks * (p.sink_blocks * us + (p.nkb - p.sink_blocks) * ur);
-  long long per = total / 1024;  // (512 workgroups at a time: a part is half of what one gets in all, at most)
+  const bool packed = a.rk.cu != nullptr;
+  const long long nkb = (a.rk.most + 63) / 64, most = (a.rq.most + 31) / 32 + 1;
+  p.heads = packed ? a.Hkv : a.B * a.Hkv;
+  p.blocks = (int)(packed ? win_blocks(a.rk, a.B) : nkb);
+  const long long run = m.left < 0 || m.right < 0 ? most : ((long long)(m.left + m.right + 2) * m.unit + 64) / 32 + 2;
+  const long long ur = (run < most ? run : most) * a.G, us = most * a.G;
+  const long long sb = run < most ? ((long long)m.sinks * m.unit + 63) / 64 : 0;
+  p.sink_blocks = (int)(sb < nkb ? sb : nkb);
+  p.sinks = p.sink_blocks ? (packed ? a.B : 1) : 0;
+  const long long sinks = (long long)p.sinks * p.sink_blocks, others = p.blocks;
+  const long long total = p.heads * (sinks * us + others * ur);
+  // 512 workgroups of two wavefronts run at a time: a part is at most half of what one gets in all
+  long long per = total / 1024;
   if (per < 32) per = 32;
   if (per > 1 << 30) per = 1 << 30;
   p.per = (int)per;
   auto parts = [&](long long units) { return (int)((units + per - 1) / per < 64 ? (units + per - 1) / per : 64); };
   p.sink_parts = p.sink_blocks ? parts(us) : 1;
-  p.parts = blocks * p.nkb >= 512 ? 1 : parts(ur);
-  if (p.sink_parts < 1) p.sink_parts = 1;
+  p.parts = p.heads * others >= 512 ? 1 : parts(ur);
   if (p.parts < 1) p.parts = 1;
-  p.slots = p.parts > 1 ? p.items() : p.sink_parts > 1 ? p.sink_blocks * p.sink_parts : 0;
+  p.per_head = (int)(p.sink_items() + others * p.parts);
+  p.slots = p.parts > 1 ? p.per_head : p.sink_parts > 1 ? p.sink_items() : 0;
+  p.nw = (long long)p.heads * p.per_head <= 256 ? 4 : 2;
   return p;
 }
 
-size_t window_parts(const WinArgs& a, int d) { return (size_t)a.B * a.Hkv * dkv_plan(a).slots * (2 * 64 * d); }
+size_t window_parts(const WinArgs& a, int d) { const DkvPlan p = dkv_plan(a); return (size_t)p.heads * p.slots * (2 * 64 * d); }
 
 // dK, dV.  The products of a unit, in this order, and what lies behind their matrix instructions:
 //   S = Q K^T, from -lse / scale    copies of Q and the row terms of u + 1
@@ -508,9 +534,10 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
   __shared__ __attribute__((aligned(256))) float terms[NW][2][64];  // of a unit's 32 rows: what S starts from, dP
   __shared__ int2 seen_by[NW][64];  // queries that see a key (registers are short)
   static_assert(PLACE == 64 * D * 4, "the partial results fit the stages");
-  int b, hk, item, kblk, part, of;
-  if (!win_item(blockIdx.x, (unsigned)a.Hkv, (unsigned)plan.items(), b, hk, item)) return;
-  plan.at(item, kblk, part, of);
+  int head, item;
+  DkvItem at;
+  if (!win_item(blockIdx.x, (unsigned)plan.heads, (unsigned)plan.per_head, head, item) || !dkv_item(a, plan, head, item, at)) return;
+  const int b = at.b, hk = at.hk, kblk = at.block, part = at.part, of = at.of;
   const WinSeq sq = win_seq(a.rq, b), sk = win_seq(a.rk, b);
   const int k0 = kblk * 64, keys = min(64, sk.n - k0);
   if (keys <= 0) return;
@@ -832,7 +859,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
     else __builtin_amdgcn_wave_barrier();
     store_columns<D, F16, NW, 2>(dk, a.scale, (float*)smem, PLACE / 4, tid, keys, [&](int r) { return a.dk.out(b, sk.row0 + k0 + r, hk); });
   } else {
-    float* const slot = parts + (((long long)b * a.Hkv + hk) * plan.slots + plan.slot(kblk, part)) * (2 * 64 * D);
+    float* const slot = parts + (head * plan.slots + item) * (2 * 64 * D);
     store_part<D, NW>(dv, (float*)smem, tid, keys, slot);
     if (NW > 1) __syncthreads();
     else __builtin_amdgcn_wave_barrier();
@@ -842,15 +869,19 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
 
 // the parts of a block added in order, 8 elements a thread
 template <int D, bool F16>
-__global__ __launch_bounds__(256) void k_window_join(WinArgs a, DkvPlan plan, const float* __restrict__ parts, int blocks) {
-  const int block = blockIdx.x % blocks, bh = blockIdx.x / blocks, hk = bh % a.Hkv, b = bh / a.Hkv;
+__global__ __launch_bounds__(256) void k_window_join(WinArgs a, DkvPlan plan, const float* __restrict__ parts, int sink_blocks, int blocks) {
+  const int k = blockIdx.x % (sink_blocks + blocks), head = blockIdx.x / (sink_blocks + blocks);
+  const int item = k < sink_blocks ? k * plan.sink_parts : plan.sink_items() + (k - sink_blocks) * plan.parts;
+  DkvItem at;
+  if (!dkv_item(a, plan, head, item, at)) return;
+  const int b = at.b, hk = at.hk;
   const WinSeq sq = win_seq(a.rq, b), sk = win_seq(a.rk, b);
-  const int k0 = block * 64, keys = min(64, sk.n - k0);
+  const int k0 = at.block * 64, keys = min(64, sk.n - k0);
   if (keys <= 0) return;
   const KeyWalk walk(a.mask, k0, k0 + keys, sq.n, sk.n - sq.n, 32);
-  const int live = plan.live(walk.n * a.G, block < plan.sink_blocks ? plan.sink_parts : plan.parts);
+  const int live = plan.live(walk.n * a.G, at.of);
   if (live == 1) return;
-  const float* from = parts + (((long long)b * a.Hkv + hk) * plan.slots + plan.slot(block, 0)) * (2 * 64 * D);
+  const float* from = parts + (head * plan.slots + item) * (2 * 64 * D);
   for (int it = threadIdx.x; it < 2 * keys * (D / 8); it += 256) {
     const int which = it / (keys * (D / 8)), r = it / (D / 8) % keys, ch = it % (D / 8);
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -875,23 +906,23 @@ hipError_t launch(const WinArgs& a, float* parts, hipStream_t s) {
   if (lanes > 0) k_window_stats<D, F16><<<(unsigned)((lanes + 255) / 256), 256, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int nqb = (a.rq.most + 63) / 64;
-  if (nqb > 0) {
-    const unsigned items = (unsigned)nqb * a.H, grid = win_grid(a.B, items);
-    if ((long long)items * a.B <= 512) k_window_dq<D, F16, 4><<<grid, 256, 0, s>>>(a, nqb);
-    else k_window_dq<D, F16, 1><<<grid, 64, 0, s>>>(a, nqb);
+  if (a.rq.most > 0) {
+    RowPlan plan = {(int)(a.rq.cu ? win_blocks(a.rq, a.B) : (a.rq.most + 63) / 64), 1, 1, 1};
+    const long long groups = win_workgroups(a, plan);
+    if (groups <= 512) k_window_dq<D, F16, 4><<<win_grid(groups), 256, 0, s>>>(a, plan);
+    else k_window_dq<D, F16, 1><<<win_grid(groups), 64, 0, s>>>(a, plan);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (a.rk.most > 0) {
     const DkvPlan plan = dkv_plan(a);
-    const unsigned items = (unsigned)plan.items() * a.Hkv, grid = win_grid(a.B, items);
-    if ((long long)items * a.B <= 256) k_window_dkv<D, F16, 4><<<grid, 256, 0, s>>>(a, plan, parts);
+    const unsigned grid = win_grid((long long)plan.heads * plan.per_head);
+    if (plan.nw == 4) k_window_dkv<D, F16, 4><<<grid, 256, 0, s>>>(a, plan, parts);
     else k_window_dkv<D, F16, 2><<<grid, 128, 0, s>>>(a, plan, parts);
     e = hipGetLastError();
     if (e != hipSuccess || plan.slots == 0) return e;
-    const int blocks = plan.parts > 1 ? plan.nkb : plan.sink_blocks;
-    k_window_join<D, F16><<<(unsigned)(blocks * a.B * a.Hkv), 256, 0, s>>>(a, plan, parts, blocks);
+    const int sinks = plan.sink_parts > 1 ? plan.sinks * plan.sink_blocks : 0, blocks = plan.parts > 1 ? plan.blocks : 0;
+    k_window_join<D, F16><<<(unsigned)(plan.heads * (sinks + blocks)), 256, 0, s>>>(a, plan, parts, sinks, blocks);
     e = hipGetLastError();
   }
   return e;

@@ -128,14 +128,12 @@ __host__ __device__ inline WinSeq win_seq(const WinRows& r, int b) {
   return {s, (int)(e - s)};
 }
 
-// Workgroup number -> sequence, key head and one of the head's `per_head` items (the items of a sequence padded up to a multiple of 8).
+// Item number `block` of a launch -> head (of `heads`) and one of its `per_head` items; false: there are fewer.
 // Workgroups are dealt to the 8 XCDs in turn, each of which has an L2.  An XCD takes whole heads, whose items read the same
-// keys; those of the heads left over are dealt to all of them, item by item, so that the XCDs get the same amount of work (16384
-// tokens, 12 heads, windows of four frames: with contiguous runs of all items a fifth of the chip's time was lost).
-__device__ __forceinline__ bool win_item(unsigned block, unsigned heads, unsigned per_head, int& b, int& head, int& item) {
-  const unsigned padded = (heads * per_head + 7u) & ~7u;
-  b = (int)(block / padded);
-  const unsigned i = block - (unsigned)b * padded, x = i & 7u, n = i >> 3, whole = heads >> 3, rest = heads & 7u;
+// keys; those of the heads left over are dealt to all of them, item by item, so that the XCDs get the same amount of work (packed
+// prompts of 1 to 6001 tokens, 16 heads on 4: with contiguous runs of a sequence's items 170 us, so 145).
+__device__ __forceinline__ bool win_item(unsigned block, unsigned heads, unsigned per_head, int& head, int& item) {
+  const unsigned x = block & 7u, n = block >> 3, whole = heads >> 3, rest = heads & 7u;
   if (n < whole * per_head) {
     const unsigned k = n / per_head;
     head = (int)(x + 8u * k);
@@ -148,7 +146,46 @@ __device__ __forceinline__ bool win_item(unsigned block, unsigned heads, unsigne
   head = (int)(8u * whole + j - (unsigned)item * rest);
   return true;
 }
-inline unsigned win_grid(int B, unsigned items) { return (unsigned)B * ((items + 7u) & ~7u); }
+inline unsigned win_grid(long long items) { return (unsigned)((items + 7) & ~7ll); }
+
+// Blocks of 64 rows of all sequences, one sequence behind the other: at most `win_blocks`.  Dense: the same number each.
+inline long long win_blocks(const WinRows& r, int B) {
+  const long long each = (r.most + 63) / 64;
+  if (!r.cu) return each * B;
+  const long long all = r.total / 64 + B;
+  return all < each * B ? all : each * B;
+}
+// block number t of all -> its sequence and number there (all lanes of a wavefront; none is launched for rows that are not there,
+// beyond one a sequence); false: there are fewer
+__device__ __forceinline__ bool win_find(const WinRows& r, int B, unsigned t, int& b, int& block) {
+  if (!r.cu) {
+    const unsigned each = (unsigned)(r.most + 63) / 64u;
+    b = (int)(t / each);
+    block = (int)(t - (unsigned)b * each);
+    return b < B;
+  }
+  const int lane = threadIdx.x & 63;
+  unsigned before = 0;
+  for (int b0 = 0; b0 < B; b0 += 64) {
+    const unsigned mine = b0 + lane < B ? (unsigned)(win_seq(r, b0 + lane).n + 63) / 64u : 0u;
+    unsigned upto = mine;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const unsigned x = __shfl_up(upto, m);
+      if (lane >= m) upto += x;
+    }
+    const unsigned long long past = __ballot(before + upto > t);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      b = __builtin_amdgcn_readfirstlane(b0 + l);
+      block = (int)(t - before) - (int)__builtin_amdgcn_readlane((int)(upto - mine), l);
+      block = __builtin_amdgcn_readfirstlane(block);
+      return true;
+    }
+    before += (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
+  }
+  return false;
+}
 
 struct WinArgs {
   WinMask mask;
@@ -162,5 +199,41 @@ struct WinArgs {
   // row of the statistics of query i of sequence b with first row row0
   __device__ long long stat(int h, int b, long long row0, int i) const { return h * lse_rows + (rq.cu ? row0 : (long long)b * rq.most) + i; }
 };
+
+// How the blocks of 64 queries are dealt to workgroups of `nw` wavefronts: each head's (dense: each sequence's and head's) `blocks`, in
+// `parts` parts of their keys of at least `per` units of 32.
+struct RowPlan {
+  int blocks, parts, per, nw;
+};
+struct RowItem {
+  int b, hk, g, qb, part;
+};
+__device__ __forceinline__ bool win_rows(const WinArgs& a, const RowPlan& plan, unsigned workgroup, RowItem& t) {
+  int head, item;
+  const bool packed = a.rq.cu != nullptr;
+  if (!win_item(workgroup, (unsigned)(packed ? a.Hkv : a.B * a.Hkv), (unsigned)(plan.blocks * a.G * plan.parts), head, item)) return false;
+  t.part = item % plan.parts;
+  item /= plan.parts;
+  t.g = item % a.G;
+  const int block = plan.blocks - 1 - item / a.G;  // (the last queries have most to walk: they come first)
+  if (packed) {
+    t.hk = head;
+    return win_find(a.rq, a.B, (unsigned)block, t.b, t.qb);
+  }
+  t.b = head / a.Hkv;
+  t.hk = head - t.b * a.Hkv;
+  t.qb = block;
+  return true;
+}
+inline long long win_workgroups(const WinArgs& a, const RowPlan& plan) {
+  return (long long)(a.rq.cu ? 1 : a.B) * a.Hkv * plan.blocks * a.G * plan.parts;
+}
+// units of 32 keys that a block of queries walks at most
+inline long long win_units(const WinMask& m, long long max_k) {
+  const long long all = max_k / 32 + 1;
+  if (m.left < 0 || m.right < 0) return all;
+  const long long run = ((long long)(m.left + m.right + 2) * m.unit + 64) / 32 + 1 + ((long long)m.sinks * m.unit + 31) / 32;
+  return run < all ? run : all;
+}
 
 }  // namespace vsa

@@ -126,7 +126,7 @@ __device__ __forceinline__ void mm_o(f32x16& acc, bf16x8 a, bf16x8 b) {
 }
 
 template <int D, bool F16, int NW, bool PAGED>
-__global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs cache, int nqb) {
+__global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs cache, RowPlan plan, float* __restrict__ parts) {
   using TL = Tile<D>;
   using TK = WinTicks<D, PAGED>;
   constexpr TK ticks;
@@ -135,9 +135,9 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
   __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * 4 * HALF];
   __shared__ float ml[NW * 64 * 2];
 
-  int b, hk, item;
-  if (!win_item(blockIdx.x, (unsigned)a.Hkv, (unsigned)(nqb * a.G), b, hk, item)) return;
-  const int g = item % a.G, qb = nqb - 1 - item / a.G, hq = hk * a.G + g;  // (the last queries have most to walk: they come first)
+  RowItem at;
+  if (!win_rows(a, plan, blockIdx.x, at)) return;
+  const int b = at.b, hk = at.hk, qb = at.qb, hq = hk * a.G + at.g;
   const WinSeq sq = win_seq(a.rq, b);
   const int r0 = qb * 64, rows = min(64, sq.n - r0);
   if (rows <= 0) return;
@@ -147,24 +147,17 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
   const int nk = __builtin_amdgcn_readfirstlane(sk.n), shift = nk - sq.n;
   WinWalk walk(a.mask, r0 + shift, r0 + rows - 1 + shift, nk, 32, PAGED ? 32 : 1);
   walk.uniform();
+  // this workgroup's part of the walk
+  const int want = (walk.n + plan.per - 1) / plan.per, live = plan.parts == 1 || want <= 1 ? 1 : want < plan.parts ? want : plan.parts;
+  if (at.part >= live) return;
+  const int begin = (int)((long long)walk.n * at.part / live), end = (int)((long long)walk.n * (at.part + 1) / live);
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, h = lane >> 5;
-  const int nu = walk.n > wave ? (walk.n - wave + NW - 1) / NW : 0;
+  const int nu = end - begin > wave ? (end - begin - wave + NW - 1) / NW : 0;
   WinSpan span[2];
 #pragma unroll
   for (int t = 0; t < 2; ++t) span[t] = win_span(a.mask, min(r0 + 32 * t + l32, sq.n - 1) + shift, nk);
-
-  // Q: of a page's operands, contraction step 2 sp + e holds elements 32 sp + 16 h + 8 e ..
-  bf16x8 qreg[2][KS];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const uint4* p = (const uint4*)a.q.row(b, sq.row0 + min(r0 + 32 * t + l32, sq.n - 1), hq);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) qreg[t][s] = __builtin_bit_cast(bf16x8, p[PAGED ? 4 * (s >> 1) + 2 * h + (s & 1) : 2 * s + h]);
-  }
-#pragma unroll
-  for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qreg[0][s]), "+v"(qreg[1][s]));  // (waited for here, ahead of the copies)
 
   const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem)) + (unsigned)wave * (4 * HALF);
   unsigned char* const mine = smem + wave * (4 * HALF);
@@ -191,7 +184,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
   };
   const float sl2 = a.scale * kLog2e;
   auto unit = [&](int u) {
-    const int i = wave + NW * min(u, nu - 1);
+    const int i = begin + wave + NW * min(u, nu - 1);
     U x;
     x.a = walk.begin(i);
     x.masked = walk.masked(i);
@@ -309,7 +302,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
     first += x.a;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const WinSpan w = walk.span_in(wave + NW * u, span[t]);
+      const WinSpan w = walk.span_in(begin + wave + NW * u, span[t]);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int key = first + (PAGED ? i : 8 * (i >> 2) + (i & 3));
@@ -367,6 +360,18 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
     copy_all(cur, false, 0);
     copy_all(n1, false, 1);
     copy_all(cur, true, 2);
+  }
+  // Q: of a page's operands, contraction step 2 sp + e holds elements 32 sp + 16 h + 8 e ..
+  bf16x8 qreg[2][KS];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const uint4* p = (const uint4*)a.q.row(b, sq.row0 + min(r0 + 32 * t + l32, sq.n - 1), hq);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qreg[t][s] = __builtin_bit_cast(bf16x8, p[PAGED ? 4 * (s >> 1) + 2 * h + (s & 1) : 2 * s + h]);
+  }
+#pragma unroll
+  for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qreg[0][s]), "+v"(qreg[1][s]));  // (requested behind the first copies, and waited for with them)
+  if (nu > 0) {
     win_wait<2 * NC>();  // K of the first unit
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -522,7 +527,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
     // units whose copies (of the next one's V and of K three on) are of 32 rows that are there: not the last of either run of keys
     int whole = nu - 1;
     if constexpr (!PAGED)
-      whole = kc.plain(nk - 32 * (walk.n_sink - 1)) && vc.plain(32) ? (walk.n - 1 - wave + NW - 1) / NW - 3 : 0;
+      whole = kc.plain(nk - 32 * (walk.n_sink - 1)) && vc.plain(32) ? (min(end, walk.n - 1) - begin - wave + NW - 1) / NW - 3 : 0;
     int u = 0;
     for (; u + 1 < whole; u += 2) {
       body(steady, even, s0, s1, u);
@@ -571,9 +576,11 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
       for (int w = 0; w < NW; ++w) L[t] += l[w] * fast_exp2(m[w] - M[t]);
     }
     const bool none = M[t] <= kUnset;
-    fac[t] = none ? 0.f : fast_exp2(own - M[t]) / L[t];
+    fac[t] = none ? 0.f : live > 1 ? fast_exp2(own - M[t]) : fast_exp2(own - M[t]) / L[t];  // (parts: normalised when they are joined)
     const int r = t * 32 + l32;
-    if (a.lse && h == 0 && wave == 0 && r < rows)
+    if (live > 1) {
+      if (h == 0 && wave == 0) *(float2*)&parts[(long long)blockIdx.x * (64 * (D + 2)) + 64 * D + 2 * r] = make_float2(M[t], L[t]);
+    } else if (a.lse && h == 0 && wave == 0 && r < rows)
       a.lse[a.stat(hq, b, sq.row0, r0 + r)] = none ? -INFINITY : (M[t] + fast_log2(L[t])) * kLn2;
   }
   float* const part = (float*)mine;
@@ -597,32 +604,129 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
       const float4 x = *(const float4*)&q[merge_offset(r, ch * 8, D)], y = *(const float4*)&q[merge_offset(r, ch * 8 + 4, D)];
       v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
     }
+    if (live > 1) {
+      float* const to = parts + (long long)blockIdx.x * (64 * (D + 2)) + r * D + ch * 8;
+      *(float4*)to = make_float4(v[0], v[1], v[2], v[3]);
+      *(float4*)(to + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      continue;
+    }
     uint4 u = {pack16<F16>(v[0], v[1]), pack16<F16>(v[2], v[3]), pack16<F16>(v[4], v[5]), pack16<F16>(v[6], v[7])};
     *((uint4*)a.o.out(b, sq.row0 + r0 + r, hq) + ch) = u;
   }
 }
 
+// The parts of a block joined in order: one workgroup a block, 8 elements a thread and turn.
+template <int D, bool F16, bool PAGED>
+__global__ __launch_bounds__(256) void k_window_merge(WinArgs a, CacheArgs cache, RowPlan plan, const float* __restrict__ parts) {
+  // (the number of the first part's workgroup: parts of a block are neighbours among the items of a head)
+  __shared__ float weight[16][64];
+  int head, item;
+  const bool packed = a.rq.cu != nullptr;
+  const unsigned heads = (unsigned)(packed ? a.Hkv : a.B * a.Hkv), per_head = (unsigned)(plan.blocks * a.G);
+  if (!win_item(blockIdx.x, heads, per_head, head, item)) return;
+  const int g = item % a.G, block = plan.blocks - 1 - item / a.G;
+  int b, hk, qb;
+  if (packed) {
+    hk = head;
+    if (!win_find(a.rq, a.B, (unsigned)block, b, qb)) return;
+  } else {
+    b = head / a.Hkv, hk = head - b * a.Hkv, qb = block;
+  }
+  const WinSeq sq = win_seq(a.rq, b);
+  const int hq = hk * a.G + g, r0 = qb * 64, rows = min(64, sq.n - r0);
+  if (rows <= 0) return;
+  const int nk = PAGED ? max(0, min(cache.lens[b], cache.max_pages * kPage)) : win_seq(a.rk, b).n, shift = nk - sq.n;
+  const WinWalk walk(a.mask, r0 + shift, r0 + rows - 1 + shift, nk, 32, PAGED ? 32 : 1);
+  const int want = (walk.n + plan.per - 1) / plan.per, live = want <= 1 ? 1 : want < plan.parts ? want : plan.parts;
+  if (live == 1) return;
+  // workgroup number of part p: the inverse of win_item
+  auto place = [&](int p) {
+    const unsigned n = (unsigned)(item * plan.parts + p), full = per_head * (unsigned)plan.parts, whole = heads >> 3, rest = heads & 7u;
+    if ((unsigned)head < 8u * whole) return ((unsigned)head >> 3) * full * 8u + n * 8u + ((unsigned)head & 7u);
+    const unsigned j = n * rest + ((unsigned)head - 8u * whole);
+    return (whole * full + (j >> 3)) * 8u + (j & 7u);
+  };
+  auto part = [&](int p) { return parts + (long long)place(p) * (64 * (D + 2)); };
+  if (threadIdx.x < (unsigned)rows) {
+    const int r = threadIdx.x;
+    float M = kUnset, L = 0.f;
+    for (int p = 0; p < live; ++p) M = fmaxf(M, part(p)[64 * D + 2 * r]);
+    for (int p = 0; p < live; ++p) {
+      const float2 ml = *(const float2*)&part(p)[64 * D + 2 * r];
+      const float w = fast_exp2(ml.x - M);
+      weight[p][r] = w;
+      L += w * ml.y;
+    }
+    const bool none = M <= kUnset;
+    for (int p = 0; p < live; ++p) weight[p][r] = none ? 0.f : weight[p][r] / L;
+    if (a.lse) a.lse[a.stat(hq, b, sq.row0, r0 + r)] = none ? -INFINITY : (M + fast_log2(L)) * kLn2;
+  }
+  __syncthreads();
+  for (int it = threadIdx.x; it < rows * (D / 8); it += 256) {
+    const int r = it / (D / 8), ch = it % (D / 8);
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < live; ++p) {
+      const float* x = part(p) + r * D + ch * 8;
+      const float4 y0 = *(const float4*)x, y1 = *(const float4*)(x + 4);
+      const float w = weight[p][r];
+      v[0] = fmaf(w, y0.x, v[0]), v[1] = fmaf(w, y0.y, v[1]), v[2] = fmaf(w, y0.z, v[2]), v[3] = fmaf(w, y0.w, v[3]);
+      v[4] = fmaf(w, y1.x, v[4]), v[5] = fmaf(w, y1.y, v[5]), v[6] = fmaf(w, y1.z, v[6]), v[7] = fmaf(w, y1.w, v[7]);
+    }
+    const uint4 u = {pack16<F16>(v[0], v[1]), pack16<F16>(v[2], v[3]), pack16<F16>(v[4], v[5]), pack16<F16>(v[6], v[7])};
+    *((uint4*)a.o.out(b, sq.row0 + r0 + r, hq) + ch) = u;
+  }
+}
+
+// Wavefronts a block and parts of its walk, by the time they would take: generations of the workgroups that fit at once (a wavefront
+// takes a SIMD, 1024 in all) times the units of one, kStart units' worth of start-up and stores each, and where there are parts what
+// writing and joining them takes.  (Times of a unit are about 0.7 us; both sides measured: ROWPLAN.)
+static RowPlan row_plan(const WinArgs& a, long long max_k, bool may_split) {
+  constexpr long long kStart = 6, kJoin = 10;
+  RowPlan best = {};
+  const long long n = win_blocks(a.rq, a.B) * a.H, units = win_units(a.mask, max_k);
+  long long least = -1;
+  for (int nw = 1; nw <= 4; nw *= 4)
+    for (int p = 1; p <= (may_split ? 16 : 1); ++p) {
+      const long long places = 1024 / nw, each = (units + nw * p - 1) / (nw * p);
+      if (p > 1 && each < 4) break;
+      const long long gens = (n * p + places - 1) / places;
+      const long long time = gens * (each + kStart + (nw > 1 ? 2 : 0)) + (p > 1 ? kJoin + n * p / 64 : 0);
+      if (least < 0 || time < least) {
+        least = time;
+        best.nw = nw, best.parts = p, best.per = (int)((units + p - 1) / p);
+      }
+    }
+  best.blocks = (int)(a.rq.cu ? win_blocks(a.rq, a.B) : (a.rq.most + 63) / 64);
+  return best;
+}
+size_t row_parts(const WinArgs& a, long long max_k, int d) {
+  const RowPlan p = row_plan(a, max_k, true);
+  return p.parts > 1 ? (size_t)win_grid(win_workgroups(a, p)) * (64 * (d + 2)) : 0;
+}
+
 namespace {
 template <int D, bool F16, bool PAGED>
-hipError_t launch(const WinArgs& a, const CacheArgs& c, hipStream_t s) {
-  const int nqb = (a.rq.most + 63) / 64;
-  const unsigned items = (unsigned)nqb * (unsigned)a.H, grid = win_grid(a.B, items);
-  const long long blocks = (long long)items * a.B;
-  if (blocks <= 512) k_window_fwd<D, F16, 4, PAGED><<<grid, 256, 0, s>>>(a, c, nqb);
-  else k_window_fwd<D, F16, 1, PAGED><<<grid, 64, 0, s>>>(a, c, nqb);
+hipError_t launch(const WinArgs& a, const CacheArgs& c, float* parts, hipStream_t s) {
+  const RowPlan plan = row_plan(a, PAGED ? (long long)c.max_pages * kPage : a.rk.most, true);
+  const unsigned grid = win_grid(win_workgroups(a, plan));
+  if (plan.nw == 4) k_window_fwd<D, F16, 4, PAGED><<<grid, 256, 0, s>>>(a, c, plan, parts);
+  else k_window_fwd<D, F16, 1, PAGED><<<grid, 64, 0, s>>>(a, c, plan, parts);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || plan.parts == 1) return e;
+  k_window_merge<D, F16, PAGED><<<win_grid(win_workgroups(a, plan) / plan.parts), 256, 0, s>>>(a, c, plan, parts);
   return hipGetLastError();
 }
 }  // namespace
 
-hipError_t launch_window_fwd(const WinArgs& a, int d, bool f16, hipStream_t s) {
+hipError_t launch_window_fwd(const WinArgs& a, int d, bool f16, float* parts, hipStream_t s) {
   const CacheArgs none = {};
-  if (d == 128) return f16 ? launch<128, true, false>(a, none, s) : launch<128, false, false>(a, none, s);
-  return f16 ? launch<64, true, false>(a, none, s) : launch<64, false, false>(a, none, s);
+  if (d == 128) return f16 ? launch<128, true, false>(a, none, parts, s) : launch<128, false, false>(a, none, parts, s);
+  return f16 ? launch<64, true, false>(a, none, parts, s) : launch<64, false, false>(a, none, parts, s);
 }
 
-hipError_t launch_cache_chunk(const WinArgs& a, const CacheArgs& c, int d, bool f16, hipStream_t s) {
-  if (d == 128) return f16 ? launch<128, true, true>(a, c, s) : launch<128, false, true>(a, c, s);
-  return f16 ? launch<64, true, true>(a, c, s) : launch<64, false, true>(a, c, s);
+hipError_t launch_cache_chunk(const WinArgs& a, const CacheArgs& c, int d, bool f16, float* parts, hipStream_t s) {
+  if (d == 128) return f16 ? launch<128, true, true>(a, c, parts, s) : launch<128, false, true>(a, c, parts, s);
+  return f16 ? launch<64, true, true>(a, c, parts, s) : launch<64, false, true>(a, c, parts, s);
 }
 
 }  // namespace vsa

@@ -23,13 +23,15 @@ struct AppendArgs {
   RowView k, v;
 };
 
-hipError_t launch_window_fwd(const WinArgs& a, int d, bool f16, hipStream_t s);
+// `parts`: row_parts(a, longest keys, d) floats
+hipError_t launch_window_fwd(const WinArgs& a, int d, bool f16, float* parts, hipStream_t s);
+size_t row_parts(const WinArgs& a, long long max_k, int d);
 // `parts`: window_parts(a, d) floats
 hipError_t launch_window_bwd(const WinArgs& a, int d, bool f16, float* parts, hipStream_t s);
 size_t window_parts(const WinArgs& a, int d);
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
-// many rows a key head: the walk of launch_window_fwd over pages
-hipError_t launch_cache_chunk(const WinArgs& a, const CacheArgs& c, int d, bool f16, hipStream_t s);
+// many rows a key head: the walk of launch_window_fwd over pages; `parts`: row_parts(a, max_pages * kPage, d) floats
+hipError_t launch_cache_chunk(const WinArgs& a, const CacheArgs& c, int d, bool f16, float* parts, hipStream_t s);
 // few rows (16 at a time): the keys split over workgroups, joined behind them.  `parts`: cache_parts(...) floats
 hipError_t launch_cache_token(const WinArgs& a, const CacheArgs& c, int d, bool f16, float* parts, hipStream_t s);
 size_t cache_parts(int B, int H, int Hkv, int d, int max_q, int max_pages);

@@ -76,8 +76,8 @@ def lib():
         L.vsa_backward.argtypes = [C.POINTER(VsaParams)] + [vp] * 17 + [C.c_size_t, vp]
         L.vsa_backward.restype = C.c_int
         # (parameters of these: the structures of window.py)
-        L.vsa_window_forward.argtypes = [vp] * 9
-        L.vsa_window_workspace_bytes.argtypes = [vp]
+        L.vsa_window_forward.argtypes = [vp] * 9 + [C.c_size_t, vp]
+        L.vsa_window_workspace_bytes.argtypes = [vp, C.c_int]
         L.vsa_window_workspace_bytes.restype = C.c_size_t
         L.vsa_window_backward.argtypes = [vp] * 13 + [C.c_size_t, vp]
         L.vsa_cache_append.argtypes = [vp] * 11

@@ -131,7 +131,7 @@ def _window_call(pb, tensors, lse, cu_q, cu_k):
             setattr(p, n, _strides(_want(t, n, sk if n in ("k", "v", "dk", "dv") else sq, pb.dtype, device), n))
         if len(_known) >= 1024:
             _known.clear()
-        known = _known[key] = (p, C.addressof(p), (pb.H, sq[0] if packed else sq[0] * sq[1]), int(lib().vsa_window_workspace_bytes(C.byref(p))))
+        known = _known[key] = (p, C.addressof(p), (pb.H, sq[0] if packed else sq[0] * sq[1]), *(int(lib().vsa_window_workspace_bytes(C.byref(p), backward)) for backward in (0, 1)))
     for n, t in zip(_NAMES, tensors):
         if t.dtype is not pb.dtype or t.device != device:
             raise ValueError(f"{n} must be {pb.dtype} on {device}, not {t.dtype} on {t.device}")
@@ -147,24 +147,38 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
-def vsa_window_workspace_bytes(pb: WindowProblem) -> int:
-    return int(lib().vsa_window_workspace_bytes(C.byref(pb.params())))
+def vsa_window_workspace_bytes(pb: WindowProblem, backward: bool) -> int:
+    return int(lib().vsa_window_workspace_bytes(C.byref(pb.params()), int(backward)))
 
 
-def vsa_window_forward(pb: WindowProblem, q, k, v, out, lse=None, cu_q=None, cu_k=None):
-    """out, lse (or None: not wanted) are written; lse is fp32 [H, rows]."""
-    call = _window_call(pb, (q, k, v, out), lse, cu_q, cu_k)
-    _run(q.device, "vsa_window_forward", call[1], q.data_ptr(), k.data_ptr(), v.data_ptr(), _at(cu_q), _at(cu_k), out.data_ptr(), _at(lse))
+def _bytes(t):
+    return 0 if t is None else t.numel() * t.element_size()
 
 
-def vsa_window_backward(pb: WindowProblem, q, k, v, out, dout, lse, dq, dk, dv, workspace, cu_q=None, cu_k=None):
-    """dq, dk, dv are written; out, lse as the forward wrote them."""
-    call = _window_call(pb, (q, k, v, out, dout, dq, dk, dv), lse, cu_q, cu_k)
-    if workspace is not None and workspace.device != q.device:
+def _workspace(t, need, device):
+    """The one given, or a new one."""
+    if t is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    if t.device != device:
         raise ValueError("the workspace must be on the tensors' device")
+    return t
+
+
+def vsa_window_forward(pb: WindowProblem, q, k, v, out, lse=None, cu_q=None, cu_k=None, workspace=None):
+    """out, lse (or None: not wanted) are written; lse is fp32 [H, rows].  Without a workspace one is allocated."""
+    call = _window_call(pb, (q, k, v, out), lse, cu_q, cu_k)
+    workspace = _workspace(workspace, call[3], q.device)
+    _run(q.device, "vsa_window_forward", call[1], q.data_ptr(), k.data_ptr(), v.data_ptr(), _at(cu_q), _at(cu_k), out.data_ptr(), _at(lse),
+         workspace.data_ptr(), _bytes(workspace))
+
+
+def vsa_window_backward(pb: WindowProblem, q, k, v, out, dout, lse, dq, dk, dv, workspace=None, cu_q=None, cu_k=None):
+    """dq, dk, dv are written; out, lse as the forward wrote them.  Without a workspace one is allocated."""
+    call = _window_call(pb, (q, k, v, out, dout, dq, dk, dv), lse, cu_q, cu_k)
+    workspace = _workspace(workspace, call[4], q.device)
     _run(q.device, "vsa_window_backward", call[1], q.data_ptr(), k.data_ptr(), v.data_ptr(), _at(cu_q), _at(cu_k), out.data_ptr(),
-         dout.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _at(workspace),
-         0 if workspace is None else workspace.numel() * workspace.element_size())
+         dout.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), workspace.data_ptr(),
+         _bytes(workspace))
 
 
 class WindowBuffers:
@@ -172,7 +186,8 @@ class WindowBuffers:
 
     def __init__(self, pb: WindowProblem, device="cuda", backward=True):
         self.pb = pb
-        if vsa_window_workspace_bytes(pb) == 0:
+        need = max(vsa_window_workspace_bytes(pb, False), vsa_window_workspace_bytes(pb, True) if backward else 0)
+        if need == 0:
             raise ValueError(f"not a problem the library takes: {pb}")
         device = torch.empty(0, device=device).device
         packed = pb.total_q > 0 or pb.total_k > 0
@@ -182,10 +197,10 @@ class WindowBuffers:
         self.lse = torch.empty((pb.H, sq[0] if packed else sq[0] * sq[1]), dtype=torch.float32, device=device)
         if backward:
             self.dq, self.dk, self.dv = new(sq), new(sk), new(sk)
-            self.workspace = torch.empty(vsa_window_workspace_bytes(pb), dtype=torch.uint8, device=device)
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
 
     def forward(self, q, k, v, cu_q=None, cu_k=None):
-        vsa_window_forward(self.pb, q, k, v, self.out, self.lse, cu_q, cu_k)
+        vsa_window_forward(self.pb, q, k, v, self.out, self.lse, cu_q, cu_k, self.workspace)
 
     def backward(self, q, k, v, dout, cu_q=None, cu_k=None):
         """Behind forward() on the same inputs."""
@@ -298,14 +313,9 @@ class PagedCache:
         self._check((q, out), table, lens, cu)
         if lse is not None:
             _whole(lse, "lse", (q.shape[-2], q.shape[0] if packed else q.shape[0] * q.shape[1]), torch.float32, self.device)
-        if workspace is None:
-            workspace, size = torch.empty(known[2], dtype=torch.uint8, device=self.device), known[2]
-        else:
-            if workspace.device != self.device:
-                raise ValueError("the workspace must be on the cache's device")
-            size = workspace.numel() * workspace.element_size()
+        workspace = _workspace(workspace, known[2], self.device)
         _run(self.device, "vsa_cache_attention", known[1], q.data_ptr(), cu.data_ptr() if packed else None, lens.data_ptr(), table.data_ptr(), *self._pool,
-                  out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), size)
+                  out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), _bytes(workspace))
         return out
 
     def workspace_bytes(self, B, H, max_q, max_pages):

@@ -193,7 +193,7 @@ def test_offsets_that_lie_stay_in_bounds():
     cu = torch.tensor([-40, 70, 20, 5000], dtype=torch.int32, device="cuda")
     outs = [torch.full((rows + 128, H, d), 3.0, dtype=BF, device="cuda") for _ in range(4)]
     lse = torch.zeros(H, rows, device="cuda")
-    ws = torch.empty(window.vsa_window_workspace_bytes(pb), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(window.vsa_window_workspace_bytes(pb, True), dtype=torch.uint8, device="cuda")
     mid = [t[64:64 + rows] for t in outs]
     window.vsa_window_forward(pb, q, k, v, mid[0], lse, cu, cu)
     window.vsa_window_backward(pb, q, k, v, mid[0], do, lse, *mid[1:], ws, cu, cu)

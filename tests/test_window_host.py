@@ -48,15 +48,16 @@ FAKE = 1 << 20  # an aligned address that is never touched: every call below is 
 def test_bad_windows_are_refused(change, status):
     p = params(**change)
     L = vsa.lib()
-    assert L.vsa_window_forward(C.byref(p), *[FAKE] * 3, None, None, FAKE, None, None) == status
+    assert L.vsa_window_forward(C.byref(p), *[FAKE] * 3, None, None, FAKE, None, FAKE, 1 << 40, None) == status
     assert L.vsa_window_backward(C.byref(p), *[FAKE] * 3, None, None, *[FAKE] * 7, 1 << 40, None) == status
-    assert L.vsa_window_workspace_bytes(C.byref(p)) == 0
+    assert L.vsa_window_workspace_bytes(C.byref(p), 0) == 0 and L.vsa_window_workspace_bytes(C.byref(p), 1) == 0
 
 
 def test_bad_pointers_strides_and_workspaces_are_refused():
     L, p = vsa.lib(), params()
-    fwd = lambda q=FAKE, k=FAKE, v=FAKE, cq=None, ck=None, o=FAKE, lse=None, p=p: L.vsa_window_forward(C.byref(p), q, k, v, cq, ck, o, lse, None)
-    assert L.vsa_window_forward(None, *[None] * 8) == -1
+    fwd = lambda q=FAKE, k=FAKE, v=FAKE, cq=None, ck=None, o=FAKE, lse=None, p=p, ws=FAKE, n=1 << 40: L.vsa_window_forward(
+        C.byref(p), q, k, v, cq, ck, o, lse, ws, n, None)
+    assert L.vsa_window_forward(None, *[None] * 8, 0, None) == -1
     assert fwd(q=None) == -1 and fwd(k=None) == -1 and fwd(v=None) == -1 and fwd(o=None) == -1
     assert fwd(q=FAKE + 8) == -4 and fwd(o=FAKE + 2) == -4 and fwd(lse=FAKE + 2) == -4
     assert fwd(cq=FAKE) == -2 and fwd(ck=FAKE) == -2  # both or neither
@@ -65,7 +66,9 @@ def test_bad_pointers_strides_and_workspaces_are_refused():
         x = params()
         setattr(x, name, window.VsaStrides(*strides))
         assert fwd(p=x) == status, name
-    need = L.vsa_window_workspace_bytes(C.byref(p))
+    need = L.vsa_window_workspace_bytes(C.byref(p), 0)
+    assert need > 0 and fwd(ws=None) == -5 and fwd(n=need - 1) == -5 and fwd(ws=FAKE + 4) == -4
+    need = L.vsa_window_workspace_bytes(C.byref(p), 1)
     bwd = lambda ws, n: L.vsa_window_backward(C.byref(p), *[FAKE] * 3, None, None, *[FAKE] * 6, ws, n, None)
     assert need >= 2 * 8 * 8 and bwd(None, need) == -5 and bwd(FAKE, need - 1) == -5 and bwd(FAKE + 4, need) == -4
 
