@@ -166,9 +166,9 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan pla
   constexpr int STAGES = 5 * HALF, PLACE = STAGES > 64 * D * 4 ? STAGES : 64 * D * 4;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * PLACE];
   RowItem at;
-  if (!win_rows(a, plan, blockIdx.x, at)) return;
+  if (!win_rows(a, plan, blockIdx.x, false, at)) return;
   const int b = at.b, hk = at.hk, qb = at.qb, hq = hk * a.G + at.g;
-  const WinSeq sq = win_seq(a.rq, b), sk = win_seq(a.rk, b);
+  const WinSeq sq = at.q, sk = at.k;
   const int r0 = qb * 64, rows = min(64, sq.n - r0);
   if (rows <= 0) return;
   const int nk = __builtin_amdgcn_readfirstlane(sk.n), shift = nk - sq.n;
@@ -214,9 +214,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan pla
   vc.init(lane, (unsigned)a.v.token);
   auto first_key = [&](int u) { return walk.begin(wave + NW * min(u, nu - 1)); };  // (units behind the last: that one again)
   auto copy_all = [&](const RowCopy<D>& c, const unsigned char* base, int key, unsigned lds) {
-    int l = lane;
-    asm volatile("" : "+v"(l));
-    c.all(base + (long long)key * c.stride, lds, l, nk - key);
+    c.all(base + (long long)key * c.stride, lds, lane, nk - key);
   };
   constexpr int kV = 3 * HALF;  // of the V stages
 
@@ -235,16 +233,22 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan pla
   int b0, b1;
   TL::transposed_lane(0, lane, b0, b1);
   auto hide = [&](f32x16 (&S)[2], int u) {
-    int first = 4 * h;
-    asm volatile("" : "+v"(first));
-    first += first_key(u);
+    const int key0 = first_key(u);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const WinSpan w = walk.span_in(wave + NW * u, span[t]);
+      int first = key0 + 4 * h;
+      asm volatile("" : "+v"(first));
+      if (w.se <= key0) {  // (no sinks among these keys)
+        const unsigned from = (unsigned)(first - w.lo), many = (unsigned)(w.hi - w.lo);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = first + 8 * (i >> 2) + (i & 3);
-        S[t][i] = key < w.hi && (key >= w.lo || key < w.se) ? S[t][i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) S[t][i] = from + (unsigned)(8 * (i >> 2) + (i & 3)) < many ? S[t][i] : -INFINITY;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = first + 8 * (i >> 2) + (i & 3);
+          S[t][i] = key < w.hi && (key >= w.lo || key < w.se) ? S[t][i] : -INFINITY;
+        }
       }
     }
   };
@@ -460,6 +464,7 @@ struct DkvPlan {
 };
 struct DkvItem {
   int b, hk, block, part, of;
+  WinSeq q, k;
 };
 // item number `item` of a head (first part of a block: `item` of the join) -> what it is; false: nothing
 __device__ __forceinline__ bool dkv_item(const WinArgs& a, const DkvPlan& plan, int head, int item, DkvItem& t) {
@@ -472,16 +477,20 @@ __device__ __forceinline__ bool dkv_item(const WinArgs& a, const DkvPlan& plan, 
     const int k = item / t.of;
     t.block = k % plan.sink_blocks;
     t.b = packed ? k / plan.sink_blocks : head / a.Hkv;
+    t.q = win_seq(a.rq, t.b);
+    t.k = win_seq(a.rk, t.b);
     return true;
   }
   t.of = plan.parts;
   t.part = (item - first) % t.of;
   const int k = (item - first) / t.of;
   if (packed) {
-    if (!win_find(a.rk, a.B, (unsigned)k, t.b, t.block)) return false;
+    if (!win_find(a.rk, &a.rq, a.B, (unsigned)k, t.b, t.block, t.k, t.q)) return false;
   } else {
     t.b = head / a.Hkv;
     t.block = k;
+    t.q = {0, a.rq.most};
+    t.k = {0, a.rk.most};
   }
   return t.block >= plan.sink_blocks;
 }
@@ -538,7 +547,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
   DkvItem at;
   if (!win_item(blockIdx.x, (unsigned)plan.heads, (unsigned)plan.per_head, head, item) || !dkv_item(a, plan, head, item, at)) return;
   const int b = at.b, hk = at.hk, kblk = at.block, part = at.part, of = at.of;
-  const WinSeq sq = win_seq(a.rq, b), sk = win_seq(a.rk, b);
+  const WinSeq sq = at.q, sk = at.k;
   const int k0 = kblk * 64, keys = min(64, sk.n - k0);
   if (keys <= 0) return;
   const int nq = __builtin_amdgcn_readfirstlane(sq.n), shift = sk.n - nq;
@@ -559,7 +568,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
     const int j = min(k0 + 32 * t + l32, sk.n - 1);
     const KeySpan w = key_span(a.mask, j);
     auto clamp = [&](long long x) { return (int)(x < 0 ? 0 : x > nq ? nq : x); };
-    if (h == 0) seen_by[wave][32 * t + l32] = make_int2(clamp(w.lo - shift), clamp(w.hi - shift));
+    if (h == 0) seen_by[wave][32 * t + l32] = make_int2(clamp(w.lo - shift), max(clamp(w.lo - shift), clamp(w.hi - shift)));
     const uint4 *p = (const uint4*)a.k.row(b, sk.row0 + j, hk), *pv = (const uint4*)a.v.row(b, sk.row0 + j, hk);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -610,14 +619,10 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
     while (at_i >= wn) at_i -= wn, ++at_g;
   };
   auto copy_q = [&](const U& x, int stage) {
-    int l = lane;
-    asm volatile("" : "+v"(l));
-    qc.all(x.qp, lds0 + stage * HALF, l, nq - x.q);
+    qc.all(x.qp, lds0 + stage * HALF, lane, nq - x.q);
   };
   auto copy_d = [&](const U& x, int stage) {
-    int l = lane;
-    asm volatile("" : "+v"(l));
-    dc.all(x.dp, lds0 + (2 + stage) * HALF, l, nq - x.q);
+    dc.all(x.dp, lds0 + (2 + stage) * HALF, lane, nq - x.q);
   };
   auto copy_terms = [&](const U& x, int stage) {
     const unsigned off = nq - x.q >= 32 ? term_off : (unsigned)min(lane & 31, nq - x.q - 1) * 4u + (lane < 32 ? 0u : plane);
@@ -764,10 +769,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
       for (int t = 0; t < 2; ++t) {
         const int2 by = seen_by[wave][32 * t + l32];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int q = first + 8 * (i >> 2) + (i & 3);
-          S[t][i] = q >= by.x && q < by.y ? S[t][i] : -INFINITY;
-        }
+        for (int i = 0; i < 16; ++i) S[t][i] = (unsigned)(first - by.x) + (unsigned)(8 * (i >> 2) + (i & 3)) < (unsigned)(by.y - by.x) ? S[t][i] : -INFINITY;
       }
     }
     auto dt_op = [&](int i) { return TL::transposed_at(ds, b0, b1, i / DVB, i % DVB); };
@@ -875,7 +877,7 @@ __global__ __launch_bounds__(256) void k_window_join(WinArgs a, DkvPlan plan, co
   DkvItem at;
   if (!dkv_item(a, plan, head, item, at)) return;
   const int b = at.b, hk = at.hk;
-  const WinSeq sq = win_seq(a.rq, b), sk = win_seq(a.rk, b);
+  const WinSeq sq = at.q, sk = at.k;
   const int k0 = at.block * 64, keys = min(64, sk.n - k0);
   if (keys <= 0) return;
   const KeyWalk walk(a.mask, k0, k0 + keys, sq.n, sk.n - sq.n, 32);

@@ -155,19 +155,26 @@ inline long long win_blocks(const WinRows& r, int B) {
   const long long all = r.total / 64 + B;
   return all < each * B ? all : each * B;
 }
-// block number t of all -> its sequence and number there (all lanes of a wavefront; none is launched for rows that are not there,
-// beyond one a sequence); false: there are fewer
-__device__ __forceinline__ bool win_find(const WinRows& r, int B, unsigned t, int& b, int& block) {
+// Block number t of all -> its sequence, number there and the rows of the sequence in the tensors of r and of `other` (null: not
+// asked for); false: there are fewer.  (All lanes of a wavefront: a lane looks at a sequence.)
+__device__ __forceinline__ WinSeq win_pick(const WinSeq& s, int lane) {
+  return {(long long)(unsigned)__builtin_amdgcn_readlane((int)s.row0, lane), __builtin_amdgcn_readlane(s.n, lane)};  // (rows are below 2^31)
+}
+__device__ __forceinline__ bool win_find(const WinRows& r, const WinRows* other, int B, unsigned t, int& b, int& block, WinSeq& rows, WinSeq& others) {
   if (!r.cu) {
     const unsigned each = (unsigned)(r.most + 63) / 64u;
     b = (int)(t / each);
     block = (int)(t - (unsigned)b * each);
+    rows = {0, r.most};
+    if (other) others = win_seq(*other, b);
     return b < B;
   }
   const int lane = threadIdx.x & 63;
   unsigned before = 0;
   for (int b0 = 0; b0 < B; b0 += 64) {
-    const unsigned mine = b0 + lane < B ? (unsigned)(win_seq(r, b0 + lane).n + 63) / 64u : 0u;
+    const int at = min(b0 + lane, B - 1);
+    const WinSeq here = win_seq(r, at), there = other ? win_seq(*other, at) : WinSeq{0, 0};
+    const unsigned mine = b0 + lane < B ? (unsigned)(here.n + 63) / 64u : 0u;
     unsigned upto = mine;
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) {
@@ -180,6 +187,8 @@ __device__ __forceinline__ bool win_find(const WinRows& r, int B, unsigned t, in
       b = __builtin_amdgcn_readfirstlane(b0 + l);
       block = (int)(t - before) - (int)__builtin_amdgcn_readlane((int)(upto - mine), l);
       block = __builtin_amdgcn_readfirstlane(block);
+      rows = win_pick(here, l);
+      if (other) others = win_pick(there, l);
       return true;
     }
     before += (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
@@ -207,8 +216,10 @@ struct RowPlan {
 };
 struct RowItem {
   int b, hk, g, qb, part;
+  WinSeq q, k;
 };
-__device__ __forceinline__ bool win_rows(const WinArgs& a, const RowPlan& plan, unsigned workgroup, RowItem& t) {
+// `paged`: the keys are not rows of a tensor
+__device__ __forceinline__ bool win_rows(const WinArgs& a, const RowPlan& plan, unsigned workgroup, bool paged, RowItem& t) {
   int head, item;
   const bool packed = a.rq.cu != nullptr;
   if (!win_item(workgroup, (unsigned)(packed ? a.Hkv : a.B * a.Hkv), (unsigned)(plan.blocks * a.G * plan.parts), head, item)) return false;
@@ -218,11 +229,13 @@ __device__ __forceinline__ bool win_rows(const WinArgs& a, const RowPlan& plan, 
   const int block = plan.blocks - 1 - item / a.G;  // (the last queries have most to walk: they come first)
   if (packed) {
     t.hk = head;
-    return win_find(a.rq, a.B, (unsigned)block, t.b, t.qb);
+    return win_find(a.rq, paged ? nullptr : &a.rk, a.B, (unsigned)block, t.b, t.qb, t.q, t.k);
   }
   t.b = head / a.Hkv;
   t.hk = head - t.b * a.Hkv;
   t.qb = block;
+  t.q = {0, a.rq.most};
+  t.k = {0, a.rk.most};
   return true;
 }
 inline long long win_workgroups(const WinArgs& a, const RowPlan& plan) {

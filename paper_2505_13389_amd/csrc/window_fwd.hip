@@ -136,14 +136,13 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
   __shared__ float ml[NW * 64 * 2];
 
   RowItem at;
-  if (!win_rows(a, plan, blockIdx.x, at)) return;
+  if (!win_rows(a, plan, blockIdx.x, PAGED, at)) return;
   const int b = at.b, hk = at.hk, qb = at.qb, hq = hk * a.G + at.g;
-  const WinSeq sq = win_seq(a.rq, b);
+  const WinSeq sq = at.q;
   const int r0 = qb * 64, rows = min(64, sq.n - r0);
   if (rows <= 0) return;
-  WinSeq sk = {0, 0};
-  if constexpr (PAGED) sk.n = max(0, min(cache.lens[b], cache.max_pages * kPage));
-  else sk = win_seq(a.rk, b);
+  WinSeq sk = at.k;
+  if constexpr (PAGED) sk = {0, max(0, min(cache.lens[b], cache.max_pages * kPage))};
   const int nk = __builtin_amdgcn_readfirstlane(sk.n), shift = nk - sq.n;
   WinWalk walk(a.mask, r0 + shift, r0 + rows - 1 + shift, nk, 32, PAGED ? 32 : 1);
   walk.uniform();
@@ -213,10 +212,8 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
 #pragma unroll
       for (int c = 0; c < NC; ++c) win_copy16(of_v ? x.v : x.k, of_v ? pc.vo[c] : pc.ko[c], lds + c * 1024);
     } else {
-      int l = lane;
-      asm volatile("" : "+v"(l));  // (nothing of this is kept in registers through the walk)
-      if (of_v) vc.all(x.v, lds, l, nk - x.a);
-      else kc.all(x.k, lds, l, nk - x.a);
+      if (of_v) vc.all(x.v, lds, lane, nk - x.a);
+      else kc.all(x.k, lds, lane, nk - x.a);
     }
   };
   auto copy_aim = [&](bool of_v, int stage, int c) {
@@ -297,16 +294,21 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
     return max_across_halves(fmaxf(m, S[15]));
   };
   auto hide = [&](f32x16 (&S)[2], const U& x, int u) {  // what a query does not see
-    int first = PAGED ? 16 * h : 4 * h;
-    asm volatile("" : "+v"(first));
-    first += x.a;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const WinSpan w = walk.span_in(begin + wave + NW * u, span[t]);
+      int first = x.a + (PAGED ? 16 * h : 4 * h);
+      asm volatile("" : "+v"(first));  // (nothing of this is kept in registers through the walk)
+      if (w.se <= x.a) {  // (no sinks among these keys)
+        const unsigned from = (unsigned)(first - w.lo), many = (unsigned)(w.hi - w.lo);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = first + (PAGED ? i : 8 * (i >> 2) + (i & 3));
-        S[t][i] = key < w.hi && (key >= w.lo || key < w.se) ? S[t][i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) S[t][i] = from + (unsigned)(PAGED ? i : 8 * (i >> 2) + (i & 3)) < many ? S[t][i] : -INFINITY;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = first + (PAGED ? i : 8 * (i >> 2) + (i & 3));
+          S[t][i] = key < w.hi && (key >= w.lo || key < w.se) ? S[t][i] : -INFINITY;
+        }
       }
     }
   };
@@ -395,45 +397,43 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
 
   // Unit u, whose S is there: P(u) while S(u + 1) is multiplied into T, then PV(u) while P(u + 1) begins.  K(u + 1) has landed, K(u + 2) and
   // V(u) are on their way; V(u + 1) is requested during the first phase, K(u + 3) during the second.
-  // KIND 2: copies piece by piece; 1: at once (rows that are not there are among them); 0: u is the last unit.
-  auto body = [&](auto kind_tag, auto par_tag, f32x16 (&S)[2], f32x16 (&T)[2], int u) {
-    constexpr int KIND = decltype(kind_tag)::value;
-    constexpr bool more = KIND > 0;
-    constexpr int par = decltype(par_tag)::value;
-    constexpr int kn = 1 - par, vn = 3 - par, vc_ = 2 + par;  // stages: K(u + 1) and then K(u + 3), V(u + 1), V(u)
+  // STEADY: copies piece by piece, of rows that are there; else at once, and u may be the last unit (then what is made of the one behind
+  // it is not used).  `par` = u & 1 (a constant in the unrolled loop).
+  auto body = [&](auto steady_tag, int par, f32x16 (&S)[2], f32x16 (&T)[2], int u) {
+    constexpr bool STEADY = decltype(steady_tag)::value;
+    const int kn = 1 - par, vn = 3 - par, vc_ = 2 + par;  // stages: K(u + 1) and then K(u + 3), V(u + 1), V(u)
     KRaw kr[NK];
     VRaw vr[NV];
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) kr[i] = kcur[i];
     const float sub[2] = {ref[0] - cur.lv, ref[1] - cur.lv};
     U n3 = {};
-    if (KIND == 1) copy_all(n1, true, vn);
+    if (!STEADY) copy_all(n1, true, vn);
     bf16x8 kop;
     __builtin_amdgcn_sched_barrier(0);
     in_steps<PH>([&](auto number) {
       constexpr int j = decltype(number)::value, s = j >> 1;
-      constexpr bool copies = KIND == 2 && j % kEvery == 0 && j / kEvery < NC;
+      constexpr bool copies = STEADY && j % kEvery == 0 && j / kEvery < NC;
       if (copies) copy_aim(true, vn, j / kEvery);
-      if (j % 2 == 0 && more) kop = k_op(kr[PAGED ? s / 2 : s], s);
-      if (more) T[j & 1] = mm32<F16>(kop, qreg[j & 1][s], s == 0 ? zero16 : T[j & 1]);
+      if (j % 2 == 0) kop = k_op(kr[PAGED ? s / 2 : s], s);
+      T[j & 1] = mm32<F16>(kop, qreg[j & 1][s], s == 0 ? zero16 : T[j & 1]);
       __builtin_amdgcn_sched_barrier(0);
       if (copies) copy_piece(n1, true, j / kEvery);
       if (j == PH - 2 * kAhead) {  // V(u) has landed; newer: K(u + 2) and what has been requested of V(u + 1)
         constexpr int part = (PH - 2 * kAhead) / kEvery + 1 < NC ? (PH - 2 * kAhead) / kEvery + 1 : NC;
-        if constexpr (more) win_wait<NC + (KIND == 2 ? part : NC)>();
-        else win_wait<NC>();
+        win_wait<NC + (STEADY ? part : NC)>();
         if (PAGED && cur.a + 32 > nk) clear_tail(cur, vc_);
       }
       // operands kAhead steps further on
       if constexpr (j % 2 == 0) {
         constexpr int to = s + kAhead;
         if constexpr (to < KS) {
-          if constexpr (more && !(PAGED && to % 2)) kr[PAGED ? to / 2 : to] = read_k(kn, PAGED ? to / 2 : to);
+          if constexpr (!(PAGED && to % 2)) kr[PAGED ? to / 2 : to] = read_k(kn, PAGED ? to / 2 : to);
         } else if constexpr (to - KS < NV) {
           vr[to - KS] = read_v(vc_, to - KS);
         }
       }
-      if (j == 1 && more) n3 = unit(u + 3);
+      if (j == 1) n3 = unit(u + 3);
       p_ops(S, std::integral_constant<int, ticks.ahead[TK::in_s(j)]>{}, std::integral_constant<int, ticks.ahead[TK::in_s(j + 1)]>{}, cur.f, sub);
       __builtin_amdgcn_sched_barrier(0);
       if (j == PH - 2) {
@@ -479,30 +479,30 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
         __builtin_amdgcn_sched_barrier(0);
       }
     });
-    if (more && __builtin_expect(n1.masked, 0)) hide(T, n1, u + 1);
+    if (__builtin_expect(n1.masked, 0)) hide(T, n1, u + 1);
     const uint4 p[2][2] = {{pb[0][0], pb[0][1]}, {pb[1][0], pb[1][1]}};
     const float sub1[2] = {ref[0] - n1.lv, ref[1] - n1.lv};
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (K(u + 1) has been read: its stage may be filled; of V only what is used next is waited for early)
-    if (KIND == 1) copy_all(n3, false, kn);
+    if (!STEADY) copy_all(n3, false, kn);
     bf16x8 vop = v_op(vr[0], 0), vop1;
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_nop 1");  // (two wait states between the operands and the first matrix instruction)
     in_steps<PH>([&](auto number) {
       constexpr int j = decltype(number)::value, i = j >> 1;
-      constexpr bool copies = KIND == 2 && j % kEvery == 0 && j / kEvery < NC;
+      constexpr bool copies = STEADY && j % kEvery == 0 && j / kEvery < NC;
       if (copies) copy_aim(false, kn, j / kEvery);
       mm_o<D, F16>(o[i % DVB][j & 1], vop, __builtin_bit_cast(bf16x8, p[j & 1][i / DVB]));
       __builtin_amdgcn_sched_barrier(0);
       if (copies) copy_piece(n3, false, j / kEvery);
-      if (more && j == PH - 2 * kAhead) {  // K(u + 2) has landed; newer: V(u + 1) and what has been requested of K(u + 3)
+      if (j == PH - 2 * kAhead) {  // K(u + 2) has landed; newer: V(u + 1) and what has been requested of K(u + 3)
         constexpr int part = (PH - 2 * kAhead) / kEvery + 1 < NC ? (PH - 2 * kAhead) / kEvery + 1 : NC;
-        win_wait<NC + (KIND == 2 ? part : NC)>();
+        win_wait<NC + (STEADY ? part : NC)>();
       }
       if constexpr (j % 2 == 0) {
         constexpr int to = i + kAhead;
         if constexpr (to < KS) {
           if constexpr (to < NV) vr[to] = read_v(vc_, to);
-        } else if constexpr (more && !(PAGED && (to - KS) % 2)) {
+        } else if constexpr (!(PAGED && (to - KS) % 2)) {
           kcur[PAGED ? (to - KS) / 2 : to - KS] = read_k(par, PAGED ? (to - KS) / 2 : to - KS);
         }
         if constexpr (i + 1 < KS) {
@@ -512,37 +512,29 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
       } else {
         vop = vop1;
       }
-      if (more) p_ops(T, std::integral_constant<int, ticks.ahead[TK::in_pv(j)]>{}, std::integral_constant<int, ticks.ahead[TK::in_pv(j + 1)]>{}, n1.f, sub1);
+      p_ops(T, std::integral_constant<int, ticks.ahead[TK::in_pv(j)]>{}, std::integral_constant<int, ticks.ahead[TK::in_pv(j + 1)]>{}, n1.f, sub1);
       __builtin_amdgcn_sched_barrier(0);
     });
-    if (D == 128 && KIND < 2) mfma_fence();  // (O may be moved to other registers between one form of this and another)
+    if (D == 128 && !STEADY) mfma_fence();  // (O may be moved to other registers between one form of this and another)
     cur = n1;
     n1 = n2;
     n2 = n3;
   };
   if (nu > 0) {
-    const std::integral_constant<int, 0> even, last;
-    const std::integral_constant<int, 1> odd, edge;
-    const std::integral_constant<int, 2> steady;
     // units whose copies (of the next one's V and of K three on) are of 32 rows that are there: not the last of either run of keys
     int whole = nu - 1;
     if constexpr (!PAGED)
       whole = kc.plain(nk - 32 * (walk.n_sink - 1)) && vc.plain(32) ? (min(end, walk.n - 1) - begin - wave + NW - 1) / NW - 3 : 0;
     int u = 0;
     for (; u + 1 < whole; u += 2) {
-      body(steady, even, s0, s1, u);
-      body(steady, odd, s1, s0, u + 1);
+      body(std::true_type{}, 0, s0, s1, u);
+      body(std::true_type{}, 1, s1, s0, u + 1);
     }
     if (D == 128) mfma_fence();
-    for (; u + 2 < nu; u += 2) {
-      body(edge, even, s0, s1, u);
-      body(edge, odd, s1, s0, u + 1);
-    }
-    if (u + 1 < nu) {
-      body(edge, even, s0, s1, u);
-      body(last, odd, s1, s0, u + 1);
-    } else {
-      body(last, even, s0, s1, u);
+    for (; u < nu; ++u) {
+      body(std::false_type{}, u & 1, s0, s1, u);
+      s0[0] = s1[0];
+      s0[1] = s1[1];
     }
     win_wait<0>();  // (the copies made for units behind the last one land before their place is used again)
   }
@@ -626,16 +618,16 @@ __global__ __launch_bounds__(256) void k_window_merge(WinArgs a, CacheArgs cache
   if (!win_item(blockIdx.x, heads, per_head, head, item)) return;
   const int g = item % a.G, block = plan.blocks - 1 - item / a.G;
   int b, hk, qb;
+  WinSeq sq = {0, a.rq.most}, sk = {0, a.rk.most};
   if (packed) {
     hk = head;
-    if (!win_find(a.rq, a.B, (unsigned)block, b, qb)) return;
+    if (!win_find(a.rq, PAGED ? nullptr : &a.rk, a.B, (unsigned)block, b, qb, sq, sk)) return;
   } else {
     b = head / a.Hkv, hk = head - b * a.Hkv, qb = block;
   }
-  const WinSeq sq = win_seq(a.rq, b);
   const int hq = hk * a.G + g, r0 = qb * 64, rows = min(64, sq.n - r0);
   if (rows <= 0) return;
-  const int nk = PAGED ? max(0, min(cache.lens[b], cache.max_pages * kPage)) : win_seq(a.rk, b).n, shift = nk - sq.n;
+  const int nk = PAGED ? max(0, min(cache.lens[b], cache.max_pages * kPage)) : sk.n, shift = nk - sq.n;
   const WinWalk walk(a.mask, r0 + shift, r0 + rows - 1 + shift, nk, 32, PAGED ? 32 : 1);
   const int want = (walk.n + plan.per - 1) / plan.per, live = want <= 1 ? 1 : want < plan.parts ? want : plan.parts;
   if (live == 1) return;
@@ -678,16 +670,16 @@ __global__ __launch_bounds__(256) void k_window_merge(WinArgs a, CacheArgs cache
 }
 
 // Wavefronts a block and parts of its walk, by the time they would take: generations of the workgroups that fit at once (a wavefront
-// takes a SIMD, 1024 in all) times the units of one, kStart units' worth of start-up and stores each, and where there are parts what
+// takes a SIMD, 1024 in all; d = 64: half of one) times the units of one, kStart units' worth of start-up and stores each, and where there are parts what
 // writing and joining them takes.  (Times of a unit are about 0.7 us; both sides measured: ROWPLAN.)
-static RowPlan row_plan(const WinArgs& a, long long max_k, bool may_split) {
+static RowPlan row_plan(const WinArgs& a, long long max_k, int d) {
   constexpr long long kStart = 6, kJoin = 10;
   RowPlan best = {};
   const long long n = win_blocks(a.rq, a.B) * a.H, units = win_units(a.mask, max_k);
   long long least = -1;
   for (int nw = 1; nw <= 4; nw *= 4)
-    for (int p = 1; p <= (may_split ? 16 : 1); ++p) {
-      const long long places = 1024 / nw, each = (units + nw * p - 1) / (nw * p);
+    for (int p = 1; p <= 16; ++p) {
+      const long long places = (d == 64 ? 2048 : 1024) / nw, each = (units + nw * p - 1) / (nw * p);
       if (p > 1 && each < 4) break;
       const long long gens = (n * p + places - 1) / places;
       const long long time = gens * (each + kStart + (nw > 1 ? 2 : 0)) + (p > 1 ? kJoin + n * p / 64 : 0);
@@ -700,14 +692,14 @@ static RowPlan row_plan(const WinArgs& a, long long max_k, bool may_split) {
   return best;
 }
 size_t row_parts(const WinArgs& a, long long max_k, int d) {
-  const RowPlan p = row_plan(a, max_k, true);
+  const RowPlan p = row_plan(a, max_k, d);
   return p.parts > 1 ? (size_t)win_grid(win_workgroups(a, p)) * (64 * (d + 2)) : 0;
 }
 
 namespace {
 template <int D, bool F16, bool PAGED>
 hipError_t launch(const WinArgs& a, const CacheArgs& c, float* parts, hipStream_t s) {
-  const RowPlan plan = row_plan(a, PAGED ? (long long)c.max_pages * kPage : a.rk.most, true);
+  const RowPlan plan = row_plan(a, PAGED ? (long long)c.max_pages * kPage : a.rk.most, D);
   const unsigned grid = win_grid(win_workgroups(a, plan));
   if (plan.nw == 4) k_window_fwd<D, F16, 4, PAGED><<<grid, 256, 0, s>>>(a, c, plan, parts);
   else k_window_fwd<D, F16, 1, PAGED><<<grid, 64, 0, s>>>(a, c, plan, parts);

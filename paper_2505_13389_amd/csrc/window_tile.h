@@ -72,6 +72,8 @@ __device__ __forceinline__ bf16x8 from_e4m3(uint32_t lo, uint32_t hi) {
 __device__ __forceinline__ void win_copy16(const void* base, unsigned voff, unsigned lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff), "s"(base), "s"(lds) : "memory", "m0");
 }
+// the same waits, ahead of a run of copies
+__device__ __forceinline__ void win_aim(unsigned lds) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 4" : : "s"(lds) : "m0", "memory"); }
 #pragma clang diagnostic pop
 template <int N>
 __device__ __forceinline__ void win_wait() {
@@ -110,10 +112,19 @@ struct RowCopy {
     if (c % 4 == 2) lds_dma16_at<2048>(g, off[c % 4]);
     if (c % 4 == 3) lds_dma16_at<3072>(g, off[c % 4]);
   }
-  // `have` rows are there: the last of them stands for those behind it
+  // all of it; `have` rows are there: the last of them stands for those behind it
   __device__ __forceinline__ void all(const unsigned char* base, unsigned lds, int lane, int have) const {
+    if (__builtin_expect(plain(have), 1)) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) win_copy16(base, at(c, lane, min(have, 32) - 1), lds + (unsigned)c * 1024u);
+      for (int c = 0; c < NC; ++c) {
+        if (c % 4 == 0) win_aim(lds + (unsigned)c * 1024u);
+        piece(base, c);
+      }
+    } else {
+      asm volatile("" : "+v"(lane));  // (nothing of this is kept in registers)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) win_copy16(base, at(c, lane, min(have, 32) - 1), lds + (unsigned)c * 1024u);
+    }
   }
 };
 
