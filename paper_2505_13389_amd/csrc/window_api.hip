@@ -14,7 +14,7 @@ using vsa::WinArgs;
 
 static_assert(VSA_PAGE_TOKENS == vsa::kPage, "the page of the header");
 
-constexpr long long kMostRows = 1ll << 30;     // of a sequence, and of a tensor: row numbers stay in 32 bits
+using vsa::kMostRows;
 constexpr long long kMostBlocks = 1ll << 23;   // workgroups of a launch: 256 threads each stay below 2^32
 constexpr int64_t kMostStride = 1 << 24;       // token strides: the byte offsets of 32 rows stay in 32 bits
 
@@ -66,7 +66,7 @@ long long stat_rows(const vsa_window_t* p, bool packed) { return packed ? p->tot
 
 WinArgs window_args(const vsa_window_t* p, bool packed, const int32_t* cu_q, const int32_t* cu_k) {
   WinArgs a = {};
-  a.mask = {p->unit, p->left, p->right, p->sinks};
+  a.mask = vsa::win_mask(p->unit, p->left, p->right, p->sinks);
   a.B = p->B, a.H = p->H, a.Hkv = p->Hkv, a.G = p->H / p->Hkv;
   a.rq = {cu_q, p->max_q, packed ? p->total_q : (long long)p->max_q};
   a.rk = {cu_k, p->max_k, packed ? p->total_k : (long long)p->max_k};
@@ -125,7 +125,7 @@ int check_cache(const vsa_cache_t* p, bool attention) {
 
 WinArgs cache_args(const vsa_cache_t* p, const int32_t* cu) {
   WinArgs a = {};
-  a.mask = {p->unit, p->left, p->right, p->sinks};
+  a.mask = vsa::win_mask(p->unit, p->left, p->right, p->sinks);
   a.B = p->B, a.H = p->H, a.Hkv = p->Hkv, a.G = p->H / p->Hkv;
   a.rq = {cu, p->max_q, cu ? p->total_q : (long long)p->max_q};
   a.lse_rows = cu ? p->total_q : (long long)p->B * p->max_q;
@@ -139,7 +139,7 @@ size_t cache_bytes(const vsa_cache_t* p, const WinArgs& a) {
 }
 
 // every visible pair once, no other unmasked: blocks of queries over keys, in pieces
-int64_t replay_queries(const vsa::WinMask& m, int nq, int nk, int block, int piece, int align) {
+int64_t replay_queries(const vsa_window_t* p, const vsa::WinMask& m, int nq, int nk, int block, int piece, int align) {
   int64_t wrong = 0;
   const int shift = nk - nq;
   std::vector<int> seen(nk);
@@ -159,10 +159,10 @@ int64_t replay_queries(const vsa::WinMask& m, int nq, int nk, int block, int pie
           if ((see && j >= nk) || (!see && !walk.masked(i))) ++wrong;
         }
       }
-      auto unit = [&](long long x) { return x >= 0 ? x / m.unit : -((-x + m.unit - 1) / m.unit); };
+      auto unit = [&](long long x) { return x >= 0 ? x / p->unit : -((-x + p->unit - 1) / p->unit); };
       for (int j = 0; j < nk; ++j) {
         const long long uj = unit(j), up = unit((long long)r + shift);
-        const bool see = (m.right < 0 || uj <= up + m.right) && (m.left < 0 || uj >= up - m.left || uj < m.sinks);
+        const bool see = (p->right < 0 || uj <= up + p->right) && (p->left < 0 || uj >= up - p->left || uj < p->sinks);
         wrong += seen[j] != (see ? 1 : 0);
       }
     }
@@ -182,9 +182,9 @@ int64_t replay_keys(const vsa::WinMask& m, int nq, int nk, int block) {
       for (int i = 0; i < walk.n; ++i) {
         const int q0 = walk.from + 32 * i;
         if (q0 < 0 || q0 >= nq) ++wrong;
-        const bool masked = (long long)q0 + shift < walk.seen_from || (long long)q0 + shift + 32 > walk.seen_to || q0 + 32 > nq;
+        const bool masked = q0 + shift < walk.seen_from || q0 + shift + 32 > walk.seen_to || q0 + 32 > nq;
         for (int q = q0; q < q0 + 32; ++q) {
-          const bool see = q < nq && (long long)q + shift >= w.lo && (long long)q + shift < w.hi;
+          const bool see = q < nq && q + shift >= w.lo && q + shift < w.hi;
           if (see) ++seen[q];
           if (!see && !masked) ++wrong;
         }
@@ -322,8 +322,8 @@ int vsa_host_window_walk(const vsa_window_t* p, int32_t nq, int32_t nk, int64_t*
   if (rc != VSA_OK) return rc;
   if (!wrong) return VSA_ERR_NULL;
   if (nq < 0 || nk < 0 || nq > 1 << 16 || nk > 1 << 16) return VSA_ERR_BAD_ARG;
-  const vsa::WinMask m = {p->unit, p->left, p->right, p->sinks};
-  *wrong = replay_queries(m, nq, nk, 64, 32, 1) + replay_queries(m, nq, nk, 64, 32, 32) + replay_queries(m, nq, nk, 3, 64, 64) +
+  const vsa::WinMask m = vsa::win_mask(p->unit, p->left, p->right, p->sinks);
+  *wrong = replay_queries(p, m, nq, nk, 64, 32, 1) + replay_queries(p, m, nq, nk, 64, 32, 32) + replay_queries(p, m, nq, nk, 3, 64, 64) +
            replay_keys(m, nq, nk, 32) + replay_keys(m, nq, nk, 64);
   return *wrong ? VSA_ERR_BAD_ARG : VSA_OK;
 }

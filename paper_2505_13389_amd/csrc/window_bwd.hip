@@ -422,8 +422,9 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan pla
     k_at = k1;
   };
   if (nu > 0) {
-    // units whose copies (two on) are of 32 rows that are there: not the last of either run of keys
-    const int whole = kc.plain(nk - 32 * (walk.n_sink - 1)) && vc.plain(32) ? (walk.n - 1 - wave + NW - 1) / NW - 2 : 0;
+    // units whose copies (two on) are of 32 rows that are there: all, or not the last of either run of keys
+    int whole = 0;
+    if (kc.plain(nk - 32 * (walk.n_sink - 1)) && vc.plain(32)) whole = nk - walk.begin(walk.n - 1) >= 32 ? nu : (walk.n - 1 - wave + NW - 1) / NW - 2;
     int u = 0;
     for (; u + 1 < whole; u += 2) {
       body(std::true_type{}, 0, s0, s1, u);
@@ -504,7 +505,7 @@ static DkvPlan dkv_plan(const WinArgs& a) {
   p.blocks = (int)(packed ? win_blocks(a.rk, a.B) : nkb);
   const long long run = m.left < 0 || m.right < 0 ? most : ((long long)(m.left + m.right + 2) * m.unit + 64) / 32 + 2;
   const long long ur = (run < most ? run : most) * a.G, us = most * a.G;
-  const long long sb = run < most ? ((long long)m.sinks * m.unit + 63) / 64 : 0;
+  const long long sb = run < most ? ((long long)m.sinks + 63) / 64 : 0;
   p.sink_blocks = (int)(sb < nkb ? sb : nkb);
   p.sinks = p.sink_blocks ? (packed ? a.B : 1) : 0;
   const long long sinks = (long long)p.sinks * p.sink_blocks, others = p.blocks;
@@ -553,7 +554,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
   const int nq = __builtin_amdgcn_readfirstlane(sq.n), shift = sk.n - nq;
   const KeyWalk walk(a.mask, k0, k0 + keys, nq, shift, 32);
   const int wn = __builtin_amdgcn_readfirstlane(walk.n), wfrom = __builtin_amdgcn_readfirstlane(walk.from);
-  auto clamp_q = [&](long long x) { return __builtin_amdgcn_readfirstlane((int)(x < 0 ? 0 : x > nq ? nq : x)); };
+  auto clamp_q = [&](int x) { return __builtin_amdgcn_readfirstlane(x < 0 ? 0 : x > nq ? nq : x); };
   const int seen_from = clamp_q(walk.seen_from - shift), seen_to = clamp_q(walk.seen_to - shift);
   const int all = wn * a.G, live = plan.live(all, of);
   if (part >= live) return;
@@ -567,7 +568,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
   for (int t = 0; t < 2; ++t) {
     const int j = min(k0 + 32 * t + l32, sk.n - 1);
     const KeySpan w = key_span(a.mask, j);
-    auto clamp = [&](long long x) { return (int)(x < 0 ? 0 : x > nq ? nq : x); };
+    auto clamp = [&](int x) { return x < 0 ? 0 : x > nq ? nq : x; };
     if (h == 0) seen_by[wave][32 * t + l32] = make_int2(clamp(w.lo - shift), max(clamp(w.lo - shift), clamp(w.hi - shift)));
     const uint4 *p = (const uint4*)a.k.row(b, sk.row0 + j, hk), *pv = (const uint4*)a.v.row(b, sk.row0 + j, hk);
 #pragma unroll

@@ -11,25 +11,46 @@
 
 namespace vsa {
 
+// Numbers of tokens and positions stay below kMostRows, so that everything here fits 32 bits.
+constexpr long long kMostRows = 1ll << 28;
+
 struct WinMask {
-  int unit, left, right, sinks;
+  int unit, left, right;  // (bounded by what any position can reach: win_mask)
+  int sinks;              // in tokens
+  uint32_t magic;         // x / unit = x * magic >> 32 + shift for 0 <= x < 2^31, unit > 1
+  int shift;
 };
+inline WinMask win_mask(int unit, int left, int right, int sinks) {
+  const long long most = kMostRows;
+  WinMask m;
+  m.unit = unit < most ? unit : (int)most;
+  const int reach = (int)(most / m.unit) + 2;
+  m.left = left < reach ? left : reach;
+  m.right = right < reach ? right : reach;
+  m.sinks = (int)((long long)sinks * unit < most ? (long long)sinks * unit : most);
+  int s = 0;
+  while ((1ll << s) < m.unit) ++s;
+  m.magic = m.unit > 1 ? (uint32_t)(((1ull << (31 + s)) + (uint64_t)m.unit - 1) / (uint64_t)m.unit) : 0;
+  m.shift = s - 1;
+  return m;
+}
+__host__ __device__ inline int win_unit(const WinMask& m, int x) {  // floor(x / unit), also of negative x
+  if (m.unit == 1) return x;
+  const uint32_t y = (uint32_t)(x < 0 ? ~x : x), q = (uint32_t)(((uint64_t)y * m.magic) >> 32) >> m.shift;
+  return x < 0 ? ~(int)q : (int)q;
+}
 
 struct WinSpan {
   int lo, hi, se;  // lo <= hi, se <= hi <= nk
 };
 
 __host__ __device__ inline WinSpan win_span(const WinMask& m, int pos, int nk) {
-  long long u = pos;
-  if (m.unit > 1) {
-    const int t = pos / m.unit;
-    u = t - (pos - t * m.unit < 0 ? 1 : 0);
-  }
-  auto clamp = [](long long x, int top) { return (int)(x < 0 ? 0 : x > top ? top : x); };
+  const int u = win_unit(m, pos);
+  auto clamp = [](int x, int top) { return x < 0 ? 0 : x > top ? top : x; };
   WinSpan s;
   s.hi = m.right < 0 ? nk : clamp((u + m.right + 1) * m.unit, nk);
   s.lo = m.left < 0 ? 0 : clamp((u - m.left) * m.unit, s.hi);
-  s.se = clamp((long long)m.sinks * m.unit, s.hi);
+  s.se = m.sinks < s.hi ? m.sinks : s.hi;
   return s;
 }
 
@@ -75,28 +96,27 @@ struct WinWalk {
 
 // Queries that see any of the keys k0 .. k1 - 1 are those of [from, to); key j is seen from position lo up to (not with) hi.
 struct KeySpan {
-  long long lo, hi;
+  int lo, hi;
 };
 __host__ __device__ inline KeySpan key_span(const WinMask& m, int j) {
-  const long long u = j / m.unit, far = 1ll << 40;
-  return {m.right < 0 ? -far : (u - m.right) * m.unit, m.left < 0 || u < m.sinks ? far : (u + m.left + 1) * m.unit};
+  const int u = win_unit(m, j), far = 1 << 30;
+  return {m.right < 0 ? -far : (u - m.right) * m.unit, m.left < 0 || j < m.sinks ? far : (u + m.left + 1) * m.unit};
 }
 struct KeyWalk {
-  int from, to, n;  // queries; pieces of `piece` of them
-  long long seen_from, seen_to;  // positions that see all of the keys
+  int from, to, n;          // queries; pieces of `piece` of them
+  int seen_from, seen_to;   // positions that see all of the keys
   __host__ __device__ KeyWalk(const WinMask& m, int k0, int k1, int nq, int shift, int piece) {
     const KeySpan a = key_span(m, k0), z = key_span(m, k1 - 1);
-    auto clamp = [&](long long x) { return (int)(x < 0 ? 0 : x > nq ? nq : x); };
+    auto clamp = [&](int x) { return x < 0 ? 0 : x > nq ? nq : x; };
     from = clamp(a.lo - shift);
     // (the first keys may be sinks and the others not)
-    const long long edge = (long long)m.sinks * m.unit, last = a.hi > z.hi ? a.hi : z.hi;
-    to = clamp(last - shift);
+    to = clamp((a.hi > z.hi ? a.hi : z.hi) - shift);
     if (to < from) to = from;
     n = (to - from + piece - 1) / piece;
     seen_from = z.lo;
     seen_to = z.hi;  // never falls from key to key behind the sinks; the first key behind them has the least
-    const long long first_other = k0 > edge ? k0 : edge;
-    if (first_other < k1) seen_to = key_span(m, (int)first_other).hi;
+    const int first_other = k0 > m.sinks ? k0 : m.sinks;
+    if (first_other < k1) seen_to = key_span(m, first_other).hi;
   }
 };
 
@@ -135,14 +155,14 @@ __host__ __device__ inline WinSeq win_seq(const WinRows& r, int b) {
 __device__ __forceinline__ bool win_item(unsigned block, unsigned heads, unsigned per_head, int& head, int& item) {
   const unsigned x = block & 7u, n = block >> 3, whole = heads >> 3, rest = heads & 7u;
   if (n < whole * per_head) {
-    const unsigned k = n / per_head;
+    const unsigned k = n < per_head ? 0u : n / per_head;
     head = (int)(x + 8u * k);
     item = (int)(n - k * per_head);
     return true;
   }
   const unsigned j = (n - whole * per_head) * 8u + x;
   if (j >= rest * per_head) return false;
-  item = (int)(j / rest);
+  item = (int)((rest & (rest - 1u)) == 0u ? j >> __builtin_ctz(rest) : j / rest);
   head = (int)(8u * whole + j - (unsigned)item * rest);
   return true;
 }
@@ -223,15 +243,15 @@ __device__ __forceinline__ bool win_rows(const WinArgs& a, const RowPlan& plan, 
   int head, item;
   const bool packed = a.rq.cu != nullptr;
   if (!win_item(workgroup, (unsigned)(packed ? a.Hkv : a.B * a.Hkv), (unsigned)(plan.blocks * a.G * plan.parts), head, item)) return false;
-  t.part = item % plan.parts;
-  item /= plan.parts;
-  t.g = item % a.G;
-  const int block = plan.blocks - 1 - item / a.G;  // (the last queries have most to walk: they come first)
+  t.part = t.g = 0;
+  if (plan.parts > 1) t.part = item % plan.parts, item /= plan.parts;
+  if (a.G > 1) t.g = item % a.G, item /= a.G;
+  const int block = plan.blocks - 1 - item;  // (the last queries have most to walk: they come first)
   if (packed) {
     t.hk = head;
     return win_find(a.rq, paged ? nullptr : &a.rk, a.B, (unsigned)block, t.b, t.qb, t.q, t.k);
   }
-  t.b = head / a.Hkv;
+  t.b = a.B > 1 ? head / a.Hkv : 0;
   t.hk = head - t.b * a.Hkv;
   t.qb = block;
   t.q = {0, a.rq.most};
@@ -245,7 +265,7 @@ inline long long win_workgroups(const WinArgs& a, const RowPlan& plan) {
 inline long long win_units(const WinMask& m, long long max_k) {
   const long long all = max_k / 32 + 1;
   if (m.left < 0 || m.right < 0) return all;
-  const long long run = ((long long)(m.left + m.right + 2) * m.unit + 64) / 32 + 1 + ((long long)m.sinks * m.unit + 31) / 32;
+  const long long run = ((long long)(m.left + m.right + 2) * m.unit + 64) / 32 + 1 + (m.sinks + 31) / 32;
   return run < all ? run : all;
 }
 

@@ -154,10 +154,6 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, h = lane >> 5;
   const int nu = end - begin > wave ? (end - begin - wave + NW - 1) / NW : 0;
-  WinSpan span[2];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) span[t] = win_span(a.mask, min(r0 + 32 * t + l32, sq.n - 1) + shift, nk);
-
   const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem)) + (unsigned)wave * (4 * HALF);
   unsigned char* const mine = smem + wave * (4 * HALF);
   const unsigned char *kb = nullptr, *vb = nullptr;
@@ -226,6 +222,26 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
     else if (of_v) vc.piece(x.v, c);
     else kc.piece(x.k, c);
   };
+
+  // The first copies and Q are requested as early as can be; what follows up to their wait is done while they are on their way.
+  U cur = {}, n1 = {}, n2 = {};
+  if (nu > 0) {
+    cur = unit(0), n1 = unit(1), n2 = unit(2);
+    copy_all(cur, false, 0);
+    copy_all(n1, false, 1);
+    copy_all(cur, true, 2);
+  }
+  // Q: of a page's operands, contraction step 2 sp + e holds elements 32 sp + 16 h + 8 e ..
+  bf16x8 qreg[2][KS];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const uint4* p = (const uint4*)a.q.row(b, sq.row0 + min(r0 + 32 * t + l32, sq.n - 1), hq);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qreg[t][s] = __builtin_bit_cast(bf16x8, p[PAGED ? 4 * (s >> 1) + 2 * h + (s & 1) : 2 * s + h]);
+  }
+  WinSpan span[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) span[t] = win_span(a.mask, min(r0 + 32 * t + l32, sq.n - 1) + shift, nk);
 
   f32x16 o[DVB][2];
   float nil = 0.f;
@@ -356,21 +372,6 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
   f32x16 s0[2], s1[2];
   constexpr int kKeep = PAGED ? kAhead / 2 : kAhead;  // K reads of a unit's first steps, made during the phase before
   KRaw kcur[kKeep];
-  U cur = {}, n1 = {}, n2 = {};
-  if (nu > 0) {
-    cur = unit(0), n1 = unit(1), n2 = unit(2);
-    copy_all(cur, false, 0);
-    copy_all(n1, false, 1);
-    copy_all(cur, true, 2);
-  }
-  // Q: of a page's operands, contraction step 2 sp + e holds elements 32 sp + 16 h + 8 e ..
-  bf16x8 qreg[2][KS];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const uint4* p = (const uint4*)a.q.row(b, sq.row0 + min(r0 + 32 * t + l32, sq.n - 1), hq);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) qreg[t][s] = __builtin_bit_cast(bf16x8, p[PAGED ? 4 * (s >> 1) + 2 * h + (s & 1) : 2 * s + h]);
-  }
 #pragma unroll
   for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qreg[0][s]), "+v"(qreg[1][s]));  // (requested behind the first copies, and waited for with them)
   if (nu > 0) {
@@ -521,10 +522,10 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
     n2 = n3;
   };
   if (nu > 0) {
-    // units whose copies (of the next one's V and of K three on) are of 32 rows that are there: not the last of either run of keys
-    int whole = nu - 1;
-    if constexpr (!PAGED)
-      whole = kc.plain(nk - 32 * (walk.n_sink - 1)) && vc.plain(32) ? (min(end, walk.n - 1) - begin - wave + NW - 1) / NW - 3 : 0;
+    // units whose copies (of the next one's V and of K three on) are of 32 rows that are there: all, or not the last of either run of keys
+    int whole = PAGED ? nu : 0;
+    if (!PAGED && kc.plain(nk - 32 * (walk.n_sink - 1)) && vc.plain(32))
+      whole = nk - walk.begin(walk.n - 1) >= 32 ? nu : (min(end, walk.n - 1) - begin - wave + NW - 1) / NW - 3;
     int u = 0;
     for (; u + 1 < whole; u += 2) {
       body(std::true_type{}, 0, s0, s1, u);
