@@ -90,12 +90,12 @@ __device__ __forceinline__ void mm_q(f32x16& d, bf16x8 a, bf16x8 q) {
 }
 
 // accumulator tiles [32 x ..][64 columns] of NW wavefronts -> rows of 16 bits, scaled; `buf`: 64 * D floats a wavefront
-template <int D, bool F16, int NW, int CT, class ROW>
-__device__ __forceinline__ void store_columns(f32x16 (&acc)[D / 32][CT], float scale, float* buf, int pitch, int tid, int rows, const ROW& row_of) {
+template <int D, bool F16, int NW, class ROW>
+__device__ __forceinline__ void store_columns(f32x16 (&acc)[D / 32][2], float scale, float* buf, int pitch, int tid, int rows, const ROW& row_of) {
   const int lane = tid & 63, wave = tid >> 6, l32 = lane & 31, h = lane >> 5;
   float* const mine = buf + wave * pitch;
 #pragma unroll
-  for (int t = 0; t < CT; ++t)
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int x = 0; x < D / 32; ++x) {
       pin_acc<D>(acc[x][t]);  // (a tile at a time in ordinary registers)
@@ -107,20 +107,11 @@ __device__ __forceinline__ void store_columns(f32x16 (&acc)[D / 32][CT], float s
     }
   if (NW > 1) __syncthreads();
   else __builtin_amdgcn_wave_barrier();
-  for (int it = tid; it < rows * (D / 8); it += 64 * NW) {
-    const int r = it / (D / 8), ch = it % (D / 8);
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float* q = buf + w * pitch;
-      const float4 x = *(const float4*)&q[merge_offset(r, ch * 8, D)], y = *(const float4*)&q[merge_offset(r, ch * 8 + 4, D)];
-      v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= scale;
-    const uint4 u = {pack16<F16>(v[0], v[1]), pack16<F16>(v[2], v[3]), pack16<F16>(v[4], v[5]), pack16<F16>(v[6], v[7])};
+  win_rows_out<D, NW>(buf, pitch, tid, rows, [&](int r, int ch, const float* v) {
+    const uint4 u = {pack16<F16>(v[0] * scale, v[1] * scale), pack16<F16>(v[2] * scale, v[3] * scale), pack16<F16>(v[4] * scale, v[5] * scale),
+                     pack16<F16>(v[6] * scale, v[7] * scale)};
     *((uint4*)row_of(r) + ch) = u;
-  }
+  });
 }
 
 // the same into a slot of partial results, [64][D] floats
@@ -141,16 +132,10 @@ __device__ __forceinline__ void store_part(f32x16 (&acc)[D / 32][2], float* buf,
     }
   if (NW > 1) __syncthreads();
   else __builtin_amdgcn_wave_barrier();
-  for (int it = tid; it < rows * (D / 4); it += 64 * NW) {
-    const int r = it / (D / 4), ch = it % (D / 4);
-    float4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float4 x = *(const float4*)&buf[w * 64 * D + merge_offset(r, ch * 4, D)];
-      v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
-    }
-    *(float4*)&slot[r * D + ch * 4] = v;
-  }
+  win_rows_out<D, NW>(buf, 64 * D, tid, rows, [&](int r, int ch, const float* v) {
+    *(float4*)&slot[r * D + ch * 8] = make_float4(v[0], v[1], v[2], v[3]);
+    *(float4*)&slot[r * D + ch * 8 + 4] = make_float4(v[4], v[5], v[6], v[7]);
+  });
 }
 
 // dQ.  The products of a unit, in this order, and what lies behind their matrix instructions:
@@ -179,6 +164,26 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan pla
   const int nu = walk.n > wave ? (walk.n - wave + NW - 1) / NW : 0;
   const float sl2 = a.scale * kLog2e;
 
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem)) + (unsigned)wave * PLACE;
+  unsigned char* const mine = smem + wave * PLACE;
+  const unsigned char* kb = (const unsigned char*)uniform_ptr(a.k.row(b, sk.row0, hk));
+  const unsigned char* vb = (const unsigned char*)uniform_ptr(a.v.row(b, sk.row0, hk));
+  RowCopy<D> kc, vc;
+  kc.init(lane, (unsigned)a.k.token);
+  vc.init(lane, (unsigned)a.v.token);
+  auto first_key = [&](int u) { return walk.begin(wave + NW * min(u, nu - 1)); };  // (units behind the last: that one again)
+  auto copy_all = [&](const RowCopy<D>& c, const unsigned char* base, int key, unsigned lds) {
+    c.all(base + (long long)key * c.stride, lds, lane, nk - key);
+  };
+  constexpr int kV = 3 * HALF;  // of the V stages
+
+  // the first copies, then Q and dO, then what can be done while they are on their way
+  if (nu > 0) {
+    copy_all(kc, kb, first_key(0), lds0);
+    copy_all(vc, vb, first_key(0), lds0 + kV);
+    copy_all(kc, kb, first_key(1), lds0 + HALF);
+    copy_all(vc, vb, first_key(1), lds0 + kV + HALF);
+  }
   WinSpan span[2];
   float from[2], minus[2];  // exponents start from, -D
   bf16x8 qreg[2][KS], dreg[2][KS];
@@ -195,29 +200,6 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan pla
       dreg[t][s] = __builtin_bit_cast(bf16x8, pd[2 * s + h]);
     }
   }
-#pragma unroll
-  for (int s = 0; s < KS; ++s)
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      if (D == 128) asm volatile("" : "+a"(qreg[t][s]));
-      else asm volatile("" : "+v"(qreg[t][s]));
-      asm volatile("" : "+v"(dreg[t][s]));
-    }
-  asm volatile("" : "+v"(from[0]), "+v"(from[1]), "+v"(minus[0]), "+v"(minus[1]));
-
-  const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem)) + (unsigned)wave * PLACE;
-  unsigned char* const mine = smem + wave * PLACE;
-  const unsigned char* kb = (const unsigned char*)uniform_ptr(a.k.row(b, sk.row0, hk));
-  const unsigned char* vb = (const unsigned char*)uniform_ptr(a.v.row(b, sk.row0, hk));
-  RowCopy<D> kc, vc;
-  kc.init(lane, (unsigned)a.k.token);
-  vc.init(lane, (unsigned)a.v.token);
-  auto first_key = [&](int u) { return walk.begin(wave + NW * min(u, nu - 1)); };  // (units behind the last: that one again)
-  auto copy_all = [&](const RowCopy<D>& c, const unsigned char* base, int key, unsigned lds) {
-    c.all(base + (long long)key * c.stride, lds, lane, nk - key);
-  };
-  constexpr int kV = 3 * HALF;  // of the V stages
-
   f32x16 acc[DVB][2];
   float nil = 0.f;
   asm volatile("" : "+v"(nil));
@@ -308,11 +290,17 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan pla
   auto after = [](unsigned x) { return x == 2u * HALF ? 0u : x + HALF; };
   auto rows_of = [&](unsigned stage, int s) { return TL::rowmajor_at(mine + stage, lane_a, s); };
   bf16x8 vcur[kAhead];
+#pragma unroll
+  for (int s = 0; s < KS; ++s)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (D == 128) asm volatile("" : "+a"(qreg[t][s]));
+      else asm volatile("" : "+v"(qreg[t][s]));
+      asm volatile("" : "+v"(dreg[t][s]));
+    }
+  asm volatile("" : "+v"(from[0]), "+v"(from[1]), "+v"(minus[0]), "+v"(minus[1]));
+
   if (nu > 0) {
-    copy_all(kc, kb, first_key(0), lds0);
-    copy_all(vc, vb, first_key(0), lds0 + kV);
-    copy_all(kc, kb, first_key(1), lds0 + HALF);
-    copy_all(vc, vb, first_key(1), lds0 + kV + HALF);
     win_wait<2 * NC>();
     in_steps<KS>([&](auto number) {
       constexpr int s = decltype(number)::value;
@@ -443,7 +431,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan pla
   for (int x = 0; x < DVB; ++x) pin_acc<D>(acc[x][0]), pin_acc<D>(acc[x][1]);
   __builtin_amdgcn_sched_barrier(0);
   if (NW > 1) __syncthreads();
-  store_columns<D, F16, NW, 2>(acc, a.scale, (float*)smem, PLACE / 4, tid, rows, [&](int r) { return a.dq.out(b, sq.row0 + r0 + r, hq); });
+  store_columns<D, F16, NW>(acc, a.scale, (float*)smem, PLACE / 4, tid, rows, [&](int r) { return a.dq.out(b, sq.row0 + r0 + r, hq); });
 }
 
 // How the key blocks of a head are cut into workgroups: a block whose queries (of all heads of the group) are more than `per` units is
@@ -857,10 +845,10 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
   __builtin_amdgcn_sched_barrier(0);
   if (NW > 1) __syncthreads();
   if (live == 1) {
-    store_columns<D, F16, NW, 2>(dv, 1.f, (float*)smem, PLACE / 4, tid, keys, [&](int r) { return a.dv.out(b, sk.row0 + k0 + r, hk); });
+    store_columns<D, F16, NW>(dv, 1.f, (float*)smem, PLACE / 4, tid, keys, [&](int r) { return a.dv.out(b, sk.row0 + k0 + r, hk); });
     if (NW > 1) __syncthreads();
     else __builtin_amdgcn_wave_barrier();
-    store_columns<D, F16, NW, 2>(dk, a.scale, (float*)smem, PLACE / 4, tid, keys, [&](int r) { return a.dk.out(b, sk.row0 + k0 + r, hk); });
+    store_columns<D, F16, NW>(dk, a.scale, (float*)smem, PLACE / 4, tid, keys, [&](int r) { return a.dk.out(b, sk.row0 + k0 + r, hk); });
   } else {
     float* const slot = parts + (head * plan.slots + item) * (2 * 64 * D);
     store_part<D, NW>(dv, (float*)smem, tid, keys, slot);

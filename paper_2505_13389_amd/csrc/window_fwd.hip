@@ -587,25 +587,18 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_fwd(WinArgs a, CacheArgs 
             make_float4(o[x][t][4 * i] * fac[t], o[x][t][4 * i + 1] * fac[t], o[x][t][4 * i + 2] * fac[t], o[x][t][4 * i + 3] * fac[t]);
   if (NW > 1) __syncthreads();
   else __builtin_amdgcn_wave_barrier();
-  for (int it = tid; it < 64 * TL::CPR; it += 64 * NW) {
-    const int r = it / TL::CPR, ch = it % TL::CPR;
-    if (r >= rows) break;
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float* q = (const float*)smem + w * 64 * D;
-      const float4 x = *(const float4*)&q[merge_offset(r, ch * 8, D)], y = *(const float4*)&q[merge_offset(r, ch * 8 + 4, D)];
-      v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
-    }
+  float* const slot = parts + (long long)blockIdx.x * (64 * (D + 2));
+  const unsigned ostride = (unsigned)a.o.token;
+  unsigned char* const orow = a.o.out(b, sq.row0 + r0, hq);
+  win_rows_out<D, NW>((const float*)smem, 64 * D, tid, rows, [&](int r, int ch, const float* v) {
     if (live > 1) {
-      float* const to = parts + (long long)blockIdx.x * (64 * (D + 2)) + r * D + ch * 8;
-      *(float4*)to = make_float4(v[0], v[1], v[2], v[3]);
-      *(float4*)(to + 4) = make_float4(v[4], v[5], v[6], v[7]);
-      continue;
+      *(float4*)&slot[r * D + ch * 8] = make_float4(v[0], v[1], v[2], v[3]);
+      *(float4*)&slot[r * D + ch * 8 + 4] = make_float4(v[4], v[5], v[6], v[7]);
+      return;
     }
-    uint4 u = {pack16<F16>(v[0], v[1]), pack16<F16>(v[2], v[3]), pack16<F16>(v[4], v[5]), pack16<F16>(v[6], v[7])};
-    *((uint4*)a.o.out(b, sq.row0 + r0 + r, hq) + ch) = u;
-  }
+    const uint4 u = {pack16<F16>(v[0], v[1]), pack16<F16>(v[2], v[3]), pack16<F16>(v[4], v[5]), pack16<F16>(v[6], v[7])};
+    *((uint4*)(orow + (size_t)((unsigned)r * ostride)) + ch) = u;
+  });
 }
 
 // The parts of a block joined in order: one workgroup a block, 8 elements a thread and turn.
