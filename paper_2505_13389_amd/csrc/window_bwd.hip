@@ -144,11 +144,12 @@ __device__ __forceinline__ void store_part(f32x16 (&acc)[D / 32][2], float* buf,
 //   dQ += K^T dS(u)    the first of P(u + 1), copies of V(u + 2)
 // K has three stages (of unit u to its end, of u + 1, of u + 2), V two.
 template <int D, bool F16, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan plan) {
+__global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void k_window_dq(WinArgs a, RowPlan plan) {
   using TL = Tile<D>;
   constexpr int KS = D / 16, DVB = D / 32, HALF = 32 * D * 2, NC = RowCopy<D>::NC, PH = 2 * KS, IPM = 16 / PH;  // softmax items a matrix instruction
   constexpr int kAhead = 2, kEvery = PH / NC, kEarly = 4;  // kEarly: items of P done in the phase before its own
-  constexpr int STAGES = 5 * HALF, PLACE = STAGES > 64 * D * 4 ? STAGES : 64 * D * 4;
+  constexpr int PLACE = D == 64 ? 4 * HALF : 5 * HALF;
+  static_assert(PLACE >= 64 * D * 4, "the partial results fit the stages");
   __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * PLACE];
   RowItem at;
   if (!win_rows(a, plan, blockIdx.x, false, at)) return;
@@ -175,7 +176,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan pla
   auto copy_all = [&](const RowCopy<D>& c, const unsigned char* base, int key, unsigned lds) {
     c.all(base + (long long)key * c.stride, lds, lane, nk - key);
   };
-  constexpr int kV = 3 * HALF;  // of the V stages
+  constexpr int kV = (D == 64 ? 2 : 3) * HALF;  // of the V stages
 
   // the first copies, then Q and dO, then what can be done while they are on their way
   if (nu > 0) {
@@ -285,11 +286,6 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan pla
       if (n > 1 && n < 18) d_cvt(dp, n - 2);
     }
   };
-  f32x16 s0[2], s1[2];
-  unsigned k_at = 0;  // stage of K(u), bytes
-  auto after = [](unsigned x) { return x == 2u * HALF ? 0u : x + HALF; };
-  auto rows_of = [&](unsigned stage, int s) { return TL::rowmajor_at(mine + stage, lane_a, s); };
-  bf16x8 vcur[kAhead];
 #pragma unroll
   for (int s = 0; s < KS; ++s)
 #pragma unroll
@@ -300,6 +296,55 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan pla
     }
   asm volatile("" : "+v"(from[0]), "+v"(from[1]), "+v"(minus[0]), "+v"(minus[1]));
 
+  if constexpr (D == 64) {
+    // Two wavefronts on a SIMD, each the vector work behind the other's products: in plain order, in half the registers.
+    for (int u = 0; u < nu; ++u) {
+      const unsigned char *ks = mine + (u & 1) * HALF, *vs = mine + kV + (u & 1) * HALF;
+      win_wait<2 * NC>();
+      f32x16 S[2], dp[2];
+#pragma unroll
+      for (int st = 0; st < KS; ++st) {
+        const bf16x8 ka = TL::rowmajor_at(ks, lane_a, st), va = TL::rowmajor_at(vs, lane_a, st);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (st == 0) mm_v_zero<D, F16>(S[t], ka, qreg[t][st]), mm_v_zero<D, F16>(dp[t], va, dreg[t][st]);
+          else mm_v<D, F16, false>(S[t], ka, qreg[t][st], S[t]), mm_v<D, F16, false>(dp[t], va, dreg[t][st], dp[t]);
+        }
+      }
+      if (__builtin_expect(walk.masked(wave + NW * u), 0)) hide(S, u);
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        bf16x8 ds[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          uint32_t w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int e = 8 * st + 2 * i;
+            const float p0 = fast_exp2(fmaf(S[t][e], sl2, from[t])), p1 = fast_exp2(fmaf(S[t][e + 1], sl2, from[t]));
+            w[i] = pack16<F16>(p0 * (dp[t][e] + minus[t]), p1 * (dp[t][e + 1] + minus[t]));
+          }
+          ds[t] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+        }
+#pragma unroll
+        for (int x = 0; x < DVB; ++x) {
+          const bf16x8 ka = TL::transposed_at(ks, b0, b1, st, x);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) mm_acc<D, F16>(acc[x][t], ka, ds[t]);
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the stages have been read and may be filled again)
+      __builtin_amdgcn_sched_barrier(0);
+      copy_all(kc, kb, first_key(u + 2), lds0 + (u & 1) * HALF);
+      copy_all(vc, vb, first_key(u + 2), lds0 + kV + (u & 1) * HALF);
+    }
+    win_wait<0>();
+  } else {
+  f32x16 s0[2], s1[2];
+  unsigned k_at = 0;  // stage of K(u), bytes
+  auto after = [](unsigned x) { return x == 2u * HALF ? 0u : x + HALF; };
+  auto rows_of = [&](unsigned stage, int s) { return TL::rowmajor_at(mine + stage, lane_a, s); };
+  bf16x8 vcur[kAhead];
   if (nu > 0) {
     win_wait<2 * NC>();
     in_steps<KS>([&](auto number) {
@@ -425,6 +470,7 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dq(WinArgs a, RowPlan pla
       s0[1] = s1[1];
     }
     win_wait<0>();
+  }
   }
   mfma_fence();
 #pragma unroll
