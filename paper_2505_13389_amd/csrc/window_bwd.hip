@@ -18,13 +18,11 @@ namespace vsa {
 template <int D, bool F16>
 __global__ __launch_bounds__(256) void k_window_stats(WinArgs a) {
   constexpr int CPR = D / 8;
-  const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) / CPR;
-  const int ch = threadIdx.x % CPR;
-  const long long n = a.lse_rows * a.H;
-  const long long row = (at < n ? at : n - 1) / a.H;  // heads of a row side by side
-  const int h = (int)((at < n ? at : n - 1) % a.H);
-  const int b = a.rq.cu ? 0 : (int)(row / a.rq.most);
-  const long long t = a.rq.cu ? row : row % a.rq.most;
+  const unsigned at = (blockIdx.x * 256u + threadIdx.x) / CPR, ch = threadIdx.x % CPR;  // (fewer than 2^32 lanes)
+  const unsigned n = (unsigned)(a.lse_rows * a.H), here = at < n ? at : n - 1, row = here / (unsigned)a.H;  // heads of a row side by side
+  const int h = (int)(here - row * (unsigned)a.H);
+  const int b = a.rq.cu || a.B == 1 ? 0 : (int)(row / (unsigned)a.rq.most);
+  const long long t = (long long)row - (long long)b * a.rq.most;
   float o[8], d[8], sum = 0.f;
   widen8<F16>(*((const uint4*)a.o.row(b, t, h) + ch), o);
   widen8<F16>(*((const uint4*)a.dout.row(b, t, h) + ch), d);
@@ -143,16 +141,20 @@ __device__ __forceinline__ void store_part(f32x16 (&acc)[D / 32][2], float* buf,
 //   S(u + 1) = K Q^T   dS(u)
 //   dQ += K^T dS(u)    the first of P(u + 1), copies of V(u + 2)
 // K has three stages (of unit u to its end, of u + 1, of u + 2), V two.
+template <int D, int NW>
+struct DqShape {
+  static constexpr int PLACE = (D == 64 ? 4 : 5) * 32 * D * 2;  // of a wavefront
+  static constexpr int LDS = NW * PLACE;
+};
 template <int D, bool F16, int NW>
-__global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void k_window_dq(WinArgs a, RowPlan plan) {
+__device__ __forceinline__ void dq_block(unsigned char* smem, const WinArgs& a, const RowPlan& plan, unsigned workgroup) {
   using TL = Tile<D>;
   constexpr int KS = D / 16, DVB = D / 32, HALF = 32 * D * 2, NC = RowCopy<D>::NC, PH = 2 * KS, IPM = 16 / PH;  // softmax items a matrix instruction
   constexpr int kAhead = 2, kEvery = PH / NC, kEarly = 4;  // kEarly: items of P done in the phase before its own
-  constexpr int PLACE = D == 64 ? 4 * HALF : 5 * HALF;
+  constexpr int PLACE = DqShape<D, NW>::PLACE;
   static_assert(PLACE >= 64 * D * 4, "the partial results fit the stages");
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * PLACE];
   RowItem at;
-  if (!win_rows(a, plan, blockIdx.x, false, at)) return;
+  if (!win_rows(a, plan, workgroup, false, at)) return;
   const int b = at.b, hk = at.hk, qb = at.qb, hq = hk * a.G + at.g;
   const WinSeq sq = at.q, sk = at.k;
   const int r0 = qb * 64, rows = min(64, sq.n - r0);
@@ -567,20 +569,25 @@ size_t window_parts(const WinArgs& a, int d) { const DkvPlan p = dkv_plan(a); re
 //   dV += dO^T P                    the rest of P, most of dS
 //   dK += Q^T dS                    the rest of dS, copies of dO(u + 2)
 // dK and dV are accumulation registers, K and V of the first 32 keys ordinary ones, V of the others is in LDS.
+template <int D, int NW>
+struct DkvShape {
+  static constexpr int HALF = 32 * D * 2, PLACE = 4 * HALF;  // 32 rows; stages of a wavefront
+  static constexpr int V = NW * PLACE, TERMS = V + HALF, SEEN = TERMS + NW * 512, LDS = SEEN + NW * 512;
+};
 template <int D, bool F16, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan plan, float* __restrict__ parts) {
+__device__ __forceinline__ void dkv_block(unsigned char* smem, const WinArgs& a, const DkvPlan& plan, float* __restrict__ parts, unsigned workgroup) {
   using TL = Tile<D>;
   constexpr int KS = D / 16, DVB = D / 32, HALF = 32 * D * 2, NC = RowCopy<D>::NC, PH = 2 * KS;
   constexpr int kAhead = 2, kEvery = PH / NC;
-  constexpr int PLACE = 4 * HALF;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * PLACE];
-  __shared__ __attribute__((aligned(1024))) unsigned char vsecond[HALF];
-  __shared__ __attribute__((aligned(256))) float terms[NW][2][64];  // of a unit's 32 rows: what S starts from, dP
-  __shared__ int2 seen_by[NW][64];  // queries that see a key (registers are short)
+  using SH = DkvShape<D, NW>;
+  constexpr int PLACE = SH::PLACE;
+  unsigned char* const vsecond = smem + SH::V;                       // V of the second 32 keys
+  float(*const terms)[2][64] = (float(*)[2][64])(smem + SH::TERMS);  // of a unit's 32 rows: what S starts from, dP
+  int2(*const seen_by)[64] = (int2(*)[64])(smem + SH::SEEN);         // queries that see a key (registers are short)
   static_assert(PLACE == 64 * D * 4, "the partial results fit the stages");
   int head, item;
   DkvItem at;
-  if (!win_item(blockIdx.x, (unsigned)plan.heads, (unsigned)plan.per_head, head, item) || !dkv_item(a, plan, head, item, at)) return;
+  if (!win_item(workgroup, (unsigned)plan.heads, (unsigned)plan.per_head, head, item) || !dkv_item(a, plan, head, item, at)) return;
   const int b = at.b, hk = at.hk, kblk = at.block, part = at.part, of = at.of;
   const WinSeq sq = at.q, sk = at.k;
   const int k0 = kblk * 64, keys = min(64, sk.n - k0);
@@ -596,26 +603,6 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, h = lane >> 5;
   const int nu = end - begin > wave ? (end - begin - wave + NW - 1) / NW : 0;
-
-  bf16x8 kreg[2][KS], vreg[KS];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int j = min(k0 + 32 * t + l32, sk.n - 1);
-    const KeySpan w = key_span(a.mask, j);
-    auto clamp = [&](int x) { return x < 0 ? 0 : x > nq ? nq : x; };
-    if (h == 0) seen_by[wave][32 * t + l32] = make_int2(clamp(w.lo - shift), max(clamp(w.lo - shift), clamp(w.hi - shift)));
-    const uint4 *p = (const uint4*)a.k.row(b, sk.row0 + j, hk), *pv = (const uint4*)a.v.row(b, sk.row0 + j, hk);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      kreg[t][s] = __builtin_bit_cast(bf16x8, p[2 * s + h]);
-      if (t == 0) vreg[s] = __builtin_bit_cast(bf16x8, pv[2 * s + h]);
-      else if (wave == 0) *(uint4*)(vsecond + TL::off(l32, 2 * s + h)) = pv[2 * s + h];
-    }
-  }
-#pragma unroll
-  for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(kreg[0][s]), "+v"(kreg[1][s]), "+v"(vreg[s]));
-  if (NW > 1) __syncthreads();
-  else __builtin_amdgcn_wave_barrier();
 
   const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem)) + (unsigned)wave * PLACE;
   const unsigned terms0 = __builtin_amdgcn_readfirstlane(lds_address(terms)) + (unsigned)wave * 512u;
@@ -664,6 +651,33 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
     lds_dma4<4>(x.st, off, terms0 + stage * 256u);
   };
 
+  // the first copies, then K and V, then what can be done while they are on their way
+  U cur = {}, n1 = {}, n2 = {};
+  if (nu > 0) {
+    unit_at(begin + wave);
+    cur = unit_here();
+    if (nu > 1) advance();
+    n1 = unit_here();
+    copy_d(cur, 0);
+    copy_q(cur, 0);
+    copy_terms(cur, 0);
+    copy_d(n1, 1);
+  }
+  bf16x8 kreg[2][KS], vreg[KS];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int j = min(k0 + 32 * t + l32, sk.n - 1);
+    const KeySpan w = key_span(a.mask, j);
+    auto clamp = [&](int x) { return x < 0 ? 0 : x > nq ? nq : x; };
+    if (h == 0) seen_by[wave][32 * t + l32] = make_int2(clamp(w.lo - shift), max(clamp(w.lo - shift), clamp(w.hi - shift)));
+    const uint4 *p = (const uint4*)a.k.row(b, sk.row0 + j, hk), *pv = (const uint4*)a.v.row(b, sk.row0 + j, hk);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      kreg[t][s] = __builtin_bit_cast(bf16x8, p[2 * s + h]);
+      if (t == 0) vreg[s] = __builtin_bit_cast(bf16x8, pv[2 * s + h]);
+      else if (wave == 0) *(uint4*)(vsecond + TL::off(l32, 2 * s + h)) = pv[2 * s + h];
+    }
+  }
   f32x16 dk[DVB][2], dv[DVB][2];
   float nil = 0.f;
   asm volatile("" : "+v"(nil));
@@ -738,17 +752,13 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
     }
     return x;
   };
-  U cur = {}, n1 = {}, n2 = {};
+#pragma unroll
+  for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(kreg[0][s]), "+v"(kreg[1][s]), "+v"(vreg[s]));
+  if (NW > 1) __syncthreads();
+  else __builtin_amdgcn_wave_barrier();
+
   bf16x8 qcur[kAhead];
   if (nu > 0) {
-    unit_at(begin + wave);
-    cur = unit_here();
-    if (nu > 1) advance();
-    n1 = unit_here();
-    copy_d(cur, 0);
-    copy_q(cur, 0);
-    copy_terms(cur, 0);
-    copy_d(n1, 1);
     win_wait<NC>();
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) qcur[s] = TL::rowmajor_at(mine, lane_a, s);
@@ -904,10 +914,31 @@ __global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan pl
   }
 }
 
+template <int D, bool F16, int NW>
+__global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void k_window_dq(WinArgs a, RowPlan plan) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[DqShape<D, NW>::LDS];
+  dq_block<D, F16, NW>(smem, a, plan, blockIdx.x);
+}
+template <int D, bool F16, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan plan, float* __restrict__ parts) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[DkvShape<D, NW>::LDS];
+  dkv_block<D, F16, NW>(smem, a, plan, parts, blockIdx.x);
+}
+// Both passes of a launch that leaves most of the chip idle, side by side: 2048 tokens, two heads, d = 64 30 us one behind the other, 17 so.
+template <int D, bool F16>
+__global__ __launch_bounds__(256, 1) void k_window_dq_dkv(WinArgs a, RowPlan rows, DkvPlan plan, float* __restrict__ parts, unsigned first) {
+  constexpr int LDS = DqShape<D, 4>::LDS > DkvShape<D, 4>::LDS ? DqShape<D, 4>::LDS : DkvShape<D, 4>::LDS;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[LDS];
+  if (blockIdx.x < first) dkv_block<D, F16, 4>(smem, a, plan, parts, blockIdx.x);
+  else dq_block<D, F16, 4>(smem, a, rows, blockIdx.x - first);
+}
+
 // the parts of a block added in order, 8 elements a thread
 template <int D, bool F16>
 __global__ __launch_bounds__(256) void k_window_join(WinArgs a, DkvPlan plan, const float* __restrict__ parts, int sink_blocks, int blocks) {
-  const int k = blockIdx.x % (sink_blocks + blocks), head = blockIdx.x / (sink_blocks + blocks);
+  constexpr int CPR = D / 8, SLICES = 2 * 64 * CPR / 256;  // workgroups a block: an item a thread
+  const int slice = blockIdx.x % SLICES, rest = blockIdx.x / SLICES;
+  const int k = rest % (sink_blocks + blocks), head = rest / (sink_blocks + blocks);
   const int item = k < sink_blocks ? k * plan.sink_parts : plan.sink_items() + (k - sink_blocks) * plan.parts;
   DkvItem at;
   if (!dkv_item(a, plan, head, item, at)) return;
@@ -918,22 +949,27 @@ __global__ __launch_bounds__(256) void k_window_join(WinArgs a, DkvPlan plan, co
   const KeyWalk walk(a.mask, k0, k0 + keys, sq.n, sk.n - sq.n, 32);
   const int live = plan.live(walk.n * a.G, at.of);
   if (live == 1) return;
-  const float* from = parts + (head * plan.slots + item) * (2 * 64 * D);
-  for (int it = threadIdx.x; it < 2 * keys * (D / 8); it += 256) {
-    const int which = it / (keys * (D / 8)), r = it / (D / 8) % keys, ch = it % (D / 8);
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const float* x = from + which * 64 * D + r * D + ch * 8;
-    for (int p = 0; p < live; ++p, x += 2 * 64 * D) {
-      const float4 y0 = *(const float4*)x, y1 = *(const float4*)(x + 4);
-      v[0] += y0.x, v[1] += y0.y, v[2] += y0.z, v[3] += y0.w, v[4] += y1.x, v[5] += y1.y, v[6] += y1.z, v[7] += y1.w;
-    }
-    if (which) {
+  const int it = slice * 256 + (int)threadIdx.x, which = it / (64 * CPR), r = it / CPR % 64, ch = it % CPR;
+  if (r >= keys) return;
+  const float* x = parts + (head * plan.slots + item) * (2 * 64 * D) + which * 64 * D + r * D + ch * 8;
+  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < live; p += 4) {  // (four parts on their way at once; added in order)
+    float4 y[4][2];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= a.scale;
+    for (int i = 0; i < 4; ++i) {
+      const float* from = x + (long long)min(p + i, live - 1) * (2 * 64 * D);
+      y[i][0] = *(const float4*)from, y[i][1] = *(const float4*)(from + 4);
     }
-    const uint4 u = {pack16<F16>(v[0], v[1]), pack16<F16>(v[2], v[3]), pack16<F16>(v[4], v[5]), pack16<F16>(v[6], v[7])};
-    *((uint4*)(which ? a.dk : a.dv).out(b, sk.row0 + k0 + r, hk) + ch) = u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p + i < live) {
+        v[0] += y[i][0].x, v[1] += y[i][0].y, v[2] += y[i][0].z, v[3] += y[i][0].w;
+        v[4] += y[i][1].x, v[5] += y[i][1].y, v[6] += y[i][1].z, v[7] += y[i][1].w;
+      }
   }
+  const float f = which ? a.scale : 1.f;
+  const uint4 u = {pack16<F16>(v[0] * f, v[1] * f), pack16<F16>(v[2] * f, v[3] * f), pack16<F16>(v[4] * f, v[5] * f), pack16<F16>(v[6] * f, v[7] * f)};
+  *((uint4*)(which ? a.dk : a.dv).out(b, sk.row0 + k0 + r, hk) + ch) = u;
 }
 
 namespace {
@@ -943,25 +979,25 @@ hipError_t launch(const WinArgs& a, float* parts, hipStream_t s) {
   if (lanes > 0) k_window_stats<D, F16><<<(unsigned)((lanes + 255) / 256), 256, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.rq.most > 0) {
-    RowPlan plan = {(int)(a.rq.cu ? win_blocks(a.rq, a.B) : (a.rq.most + 63) / 64), 1, 1, 1};
-    const long long groups = win_workgroups(a, plan);
-    if (groups <= 512) k_window_dq<D, F16, 4><<<win_grid(groups), 256, 0, s>>>(a, plan);
-    else k_window_dq<D, F16, 1><<<win_grid(groups), 64, 0, s>>>(a, plan);
+  const RowPlan rows = {(int)(a.rq.cu ? win_blocks(a.rq, a.B) : (a.rq.most + 63) / 64), 1, 1, 1};
+  const long long groups = win_workgroups(a, rows);
+  const DkvPlan plan = dkv_plan(a);
+  const long long items = (long long)plan.heads * plan.per_head;
+  if (groups > 0 && items > 0 && plan.nw == 4 && groups <= 128) {
+    k_window_dq_dkv<D, F16><<<win_grid(items) + win_grid(groups), 256, 0, s>>>(a, rows, plan, parts, win_grid(items));
+  } else {
+    if (groups > 512) k_window_dq<D, F16, 1><<<win_grid(groups), 64, 0, s>>>(a, rows);
+    else if (groups > 0) k_window_dq<D, F16, 4><<<win_grid(groups), 256, 0, s>>>(a, rows);
     e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || items == 0) return e;
+    if (plan.nw == 4) k_window_dkv<D, F16, 4><<<win_grid(items), 256, 0, s>>>(a, plan, parts);
+    else k_window_dkv<D, F16, 2><<<win_grid(items), 128, 0, s>>>(a, plan, parts);
   }
-  if (a.rk.most > 0) {
-    const DkvPlan plan = dkv_plan(a);
-    const unsigned grid = win_grid((long long)plan.heads * plan.per_head);
-    if (plan.nw == 4) k_window_dkv<D, F16, 4><<<grid, 256, 0, s>>>(a, plan, parts);
-    else k_window_dkv<D, F16, 2><<<grid, 128, 0, s>>>(a, plan, parts);
-    e = hipGetLastError();
-    if (e != hipSuccess || plan.slots == 0) return e;
-    const int sinks = plan.sink_parts > 1 ? plan.sinks * plan.sink_blocks : 0, blocks = plan.parts > 1 ? plan.blocks : 0;
-    k_window_join<D, F16><<<(unsigned)(plan.heads * (sinks + blocks)), 256, 0, s>>>(a, plan, parts, sinks, blocks);
-    e = hipGetLastError();
-  }
+  e = hipGetLastError();
+  if (e != hipSuccess || plan.slots == 0) return e;
+  const int sinks = plan.sink_parts > 1 ? plan.sinks * plan.sink_blocks : 0, blocks = plan.parts > 1 ? plan.blocks : 0;
+  k_window_join<D, F16><<<(unsigned)(plan.heads * (sinks + blocks)) * (2u * 64u * (D / 8) / 256u), 256, 0, s>>>(a, plan, parts, sinks, blocks);
+  e = hipGetLastError();
   return e;
 }
 }  // namespace
