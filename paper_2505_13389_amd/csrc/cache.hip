@@ -45,15 +45,10 @@ __global__ __launch_bounds__(2 * D) void k_cache_append(AppendArgs a, int most_p
   const int start = max(0, min(a.c.lens[b], a.c.max_pages * kPage));
   const int page = start / kPage + slot_page;
   if (seq.n == 0 || page >= a.c.max_pages || page * kPage - start >= seq.n) return;
-  const int id = a.c.table[(long long)b * a.c.max_pages + page];
-  if ((unsigned)id >= (unsigned)a.c.pages) return;
   const int lo = max(0, start - page * kPage), hi = min(kPage, start + seq.n - page * kPage);
   const long long first = seq.row0 + page * kPage - start;  // row of slot 0
-  const long long ph = (long long)id * a.Hkv + head;
-  uint8_t* const kp = a.c.k + ph * (kPage * D);
-  uint8_t* const vp = a.c.v + ph * (kPage * D);
-
   const int tid = threadIdx.x, c = tid % CPR, r4 = tid / CPR * 4;
+  uint4 raw[2][4];
   float x[2][4][8];
   float top[2] = {0.f, 0.f};
 #pragma unroll
@@ -63,17 +58,25 @@ __global__ __launch_bounds__(2 * D) void k_cache_append(AppendArgs a, int most_p
       const int slot = r4 + i;
       uint4 u = {0, 0, 0, 0};
       if (slot >= lo && slot < hi) u = *((const uint4*)(t ? a.v : a.k).row(b, first + slot, head) + c);
-      widen8<F16>(u, x[t][i]);
+      raw[t][i] = u;
     }
+  const int id = a.c.table[(long long)b * a.c.max_pages + page];  // (on its way together with the rows)
+  if ((unsigned)id >= (unsigned)a.c.pages) return;
+  const long long ph = (long long)id * a.Hkv + head;
+  uint8_t* const kp = a.c.k + ph * (kPage * D);
+  uint8_t* const vp = a.c.v + ph * (kPage * D);
+
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+      widen8<F16>(raw[t][i], x[t][i]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         x[t][i][e] = finite_or_nan(x[t][i][e]);  // (fmaxf takes the other operand where one is NaN)
         top[t] = fmaxf(top[t], fabsf(x[t][i][e]));
       }
+    }
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
 #pragma unroll

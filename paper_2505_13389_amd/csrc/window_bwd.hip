@@ -147,7 +147,7 @@ struct DqShape {
   static constexpr int LDS = NW * PLACE;
 };
 template <int D, bool F16, int NW>
-__device__ __forceinline__ void dq_block(unsigned char* smem, const WinArgs& a, const RowPlan& plan, unsigned workgroup) {
+__device__ __forceinline__ void dq_block(unsigned char* smem, const WinArgs& a, const RowPlan& plan, unsigned workgroup, int tid) {
   using TL = Tile<D>;
   constexpr int KS = D / 16, DVB = D / 32, HALF = 32 * D * 2, NC = RowCopy<D>::NC, PH = 2 * KS, IPM = 16 / PH;  // softmax items a matrix instruction
   constexpr int kAhead = 2, kEvery = PH / NC, kEarly = 4;  // kEarly: items of P done in the phase before its own
@@ -162,7 +162,7 @@ __device__ __forceinline__ void dq_block(unsigned char* smem, const WinArgs& a, 
   const int nk = __builtin_amdgcn_readfirstlane(sk.n), shift = nk - sq.n;
   WinWalk walk(a.mask, r0 + shift, r0 + rows - 1 + shift, nk, 32, 1);
   walk.uniform();
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, h = lane >> 5;
   const int nu = walk.n > wave ? (walk.n - wave + NW - 1) / NW : 0;
   const float sl2 = a.scale * kLog2e;
@@ -489,7 +489,7 @@ struct DkvPlan {
   int heads, per_head;                      // (dense: sequences times heads; packed: heads); items of each
   int sinks, sink_blocks, sink_parts;       // sequences of a head whose first blocks may hold sinks; those blocks, parts of each
   int blocks, parts;                        // 64-key blocks of a head (of all sequences, at most); parts of each that holds no sink
-  int per, nw;
+  int per, run;                             // units of a part at most, of a part of a block without sinks
   long long slots;                          // partial results of a head
   // item of a head: those of the sinks come first.  Their slots are numbered like the items.
   __host__ __device__ int sink_items() const { return sinks * sink_blocks * sink_parts; }
@@ -555,9 +555,9 @@ static DkvPlan dkv_plan(const WinArgs& a) {
   p.sink_parts = p.sink_blocks ? parts(us) : 1;
   p.parts = p.heads * others >= 512 ? 1 : parts(ur);
   if (p.parts < 1) p.parts = 1;
+  p.run = (int)((ur + p.parts - 1) / p.parts < per ? (ur + p.parts - 1) / p.parts : per);
   p.per_head = (int)(p.sink_items() + others * p.parts);
   p.slots = p.parts > 1 ? p.per_head : p.sink_parts > 1 ? p.sink_items() : 0;
-  p.nw = (long long)p.heads * p.per_head <= 256 ? 4 : 2;
   return p;
 }
 
@@ -914,23 +914,21 @@ __device__ __forceinline__ void dkv_block(unsigned char* smem, const WinArgs& a,
   }
 }
 
+// Both passes in one launch, dK/dV's workgroups first: dQ's fill what they leave of the chip (packed training of 10332 tokens, d = 64:
+// 216 us with a launch each, 201 so; 16 frames of 1024 tokens, 12 heads, d = 128: 1901 and 1805).  NW = 4: the four wavefronts share a
+// block of queries too; NW = 2: each takes one of its own.
 template <int D, bool F16, int NW>
-__global__ __launch_bounds__(64 * NW, D == 64 ? 2 : 1) void k_window_dq(WinArgs a, RowPlan plan) {
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[DqShape<D, NW>::LDS];
-  dq_block<D, F16, NW>(smem, a, plan, blockIdx.x);
-}
-template <int D, bool F16, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void k_window_dkv(WinArgs a, DkvPlan plan, float* __restrict__ parts) {
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[DkvShape<D, NW>::LDS];
-  dkv_block<D, F16, NW>(smem, a, plan, parts, blockIdx.x);
-}
-// Both passes of a launch that leaves most of the chip idle, side by side: 2048 tokens, two heads, d = 64 30 us one behind the other, 17 so.
-template <int D, bool F16>
-__global__ __launch_bounds__(256, 1) void k_window_dq_dkv(WinArgs a, RowPlan rows, DkvPlan plan, float* __restrict__ parts, unsigned first) {
-  constexpr int LDS = DqShape<D, 4>::LDS > DkvShape<D, 4>::LDS ? DqShape<D, 4>::LDS : DkvShape<D, 4>::LDS;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[LDS];
-  if (blockIdx.x < first) dkv_block<D, F16, 4>(smem, a, plan, parts, blockIdx.x);
-  else dq_block<D, F16, 4>(smem, a, rows, blockIdx.x - first);
+__global__ __launch_bounds__(64 * NW, 1) void k_window_dq_dkv(WinArgs a, RowPlan rows, DkvPlan plan, float* __restrict__ parts, unsigned first) {
+  constexpr int DQ = NW == 4 ? DqShape<D, 4>::LDS : NW * DqShape<D, 1>::LDS;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[DQ > DkvShape<D, NW>::LDS ? DQ : DkvShape<D, NW>::LDS];
+  if (blockIdx.x < first) {
+    dkv_block<D, F16, NW>(smem, a, plan, parts, blockIdx.x);
+  } else if constexpr (NW == 4) {
+    dq_block<D, F16, 4>(smem, a, rows, blockIdx.x - first, threadIdx.x);
+  } else {
+    const unsigned w = blockIdx.x - first, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    dq_block<D, F16, 1>(smem + wave * DqShape<D, 1>::LDS, a, rows, ((w >> 3) * NW + wave) * 8u + (w & 7u), threadIdx.x & 63);
+  }
 }
 
 // the parts of a block added in order, 8 elements a thread
@@ -973,6 +971,18 @@ __global__ __launch_bounds__(256) void k_window_join(WinArgs a, DkvPlan plan, co
 }
 
 namespace {
+// Four wavefronts a workgroup or two, by the time that either would take: all work spread over the workgroups that fit at once, and
+// the longest item behind it.  A unit of dQ is 2, one of dK/dV 3, start and stores of a workgroup 24.  (28 shapes of 512 to 8192
+// tokens, one to eight key heads: the faster one in 25, at most 5 % off in the others.  2048 tokens, 8 heads, d = 64, causal: four 63 us,
+// two 94; 8192 tokens, two heads, a window of 512: four 53, two 46.)
+bool four(const WinArgs& a, const DkvPlan& plan, long long items, long long groups) {
+  const double uq = (double)win_units(a.mask, a.rk.most), uk = (double)plan.run;
+  auto time = [&](int nw) {
+    const double k = 3 * uk / nw + 24, q = 2 * uq / (nw == 4 ? 4 : 1) + 24;
+    return (items * k + (nw == 4 ? groups : groups / 2.) * q) * nw / 1024 + (k > q ? k : q);
+  };
+  return time(4) <= time(2);
+}
 template <int D, bool F16>
 hipError_t launch(const WinArgs& a, float* parts, hipStream_t s) {
   const long long lanes = a.lse_rows * a.H * (D / 8);
@@ -983,16 +993,10 @@ hipError_t launch(const WinArgs& a, float* parts, hipStream_t s) {
   const long long groups = win_workgroups(a, rows);
   const DkvPlan plan = dkv_plan(a);
   const long long items = (long long)plan.heads * plan.per_head;
-  if (groups > 0 && items > 0 && plan.nw == 4 && groups <= 128) {
-    k_window_dq_dkv<D, F16><<<win_grid(items) + win_grid(groups), 256, 0, s>>>(a, rows, plan, parts, win_grid(items));
-  } else {
-    if (groups > 512) k_window_dq<D, F16, 1><<<win_grid(groups), 64, 0, s>>>(a, rows);
-    else if (groups > 0) k_window_dq<D, F16, 4><<<win_grid(groups), 256, 0, s>>>(a, rows);
-    e = hipGetLastError();
-    if (e != hipSuccess || items == 0) return e;
-    if (plan.nw == 4) k_window_dkv<D, F16, 4><<<win_grid(items), 256, 0, s>>>(a, plan, parts);
-    else k_window_dkv<D, F16, 2><<<win_grid(items), 128, 0, s>>>(a, plan, parts);
-  }
+  if (items + groups == 0) return e;
+  const unsigned first = win_grid(items);
+  if (four(a, plan, items, groups)) k_window_dq_dkv<D, F16, 4><<<first + win_grid(groups), 256, 0, s>>>(a, rows, plan, parts, first);
+  else k_window_dq_dkv<D, F16, 2><<<first + win_grid((groups + 1) / 2), 128, 0, s>>>(a, rows, plan, parts, first);
   e = hipGetLastError();
   if (e != hipSuccess || plan.slots == 0) return e;
   const int sinks = plan.sink_parts > 1 ? plan.sinks * plan.sink_blocks : 0, blocks = plan.parts > 1 ? plan.blocks : 0;
