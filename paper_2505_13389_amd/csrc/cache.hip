@@ -184,9 +184,9 @@ constexpr float kNoRow = -1e30f;
 struct TokenPlan {
   int tiles;                 // row tiles of the longest sequence
   int target, groups, grid;  // workgroups aimed at; (sequence, key head, row tile) triples; workgroups needed at most
-  int one;           // every sequence has one part, whatever its length: nothing is joined
+  int one;                   // every group is one workgroup's, whatever its length: nothing is joined
 };
-static TokenPlan token_plan(int B, int H, int Hkv, int max_q, int max_pages) {
+static TokenPlan token_plan(int B, int H, int Hkv, int d, int max_q, int max_pages) {
   const int G = H / Hkv;
   const long long groups = (long long)B * Hkv * (((long long)max_q * G + 15) / 16);
   TokenPlan p;
@@ -194,12 +194,16 @@ static TokenPlan token_plan(int B, int H, int Hkv, int max_q, int max_pages) {
   p.target = (int)(groups <= 256 ? 512 - groups : 4 * groups);
   p.tiles = (int)(((long long)max_q * G + 15) / 16);
   p.groups = (int)groups;
-  p.one = max_pages <= 4;
+  // A workgroup's eight wavefronts take 8 pages in 2.3 us (d = 128; d = 64: 1), parts of their own and the join cost 3 to 5 us whatever
+  // the lengths: 16 heads, 4 sequences, d = 128: 16 pages 11.5 us by one workgroup, 14.0 in parts, 32 pages 16.9 and 14.2.  Where the
+  // groups fill the chip by themselves one workgroup is better for longer (64 sequences, 8 key heads, 32 pages: 46 us, in parts 60),
+  // but a long sequence among short ones would be alone at the end: no further than 32.
+  p.one = (long long)max_pages * d <= (groups >= 128 ? 32 : 16) * 128;
   p.grid = p.one ? p.groups : p.target + p.groups;
   return p;
 }
 size_t cache_parts(int B, int H, int Hkv, int d, int max_q, int max_pages) {
-  const TokenPlan p = token_plan(B, H, Hkv, max_q, max_pages);
+  const TokenPlan p = token_plan(B, H, Hkv, d, max_q, max_pages);
   return p.one ? 0 : (size_t)p.grid * 16 * (d + 2) + (size_t)p.groups * 4;
 }
 // Which sequence a workgroup works for, and what of it.
@@ -235,7 +239,7 @@ __device__ __forceinline__ bool token_item(const WinArgs& a, const CacheArgs& c,
     total += (long long)p * g;
   }
   total = sum(total);
-  t.per = plan.one ? 4 : (int)max(4ll, (total / plan.target + 4) / 4 * 4);
+  t.per = (int)max(4ll, (total / plan.target + 4) / 4 * 4);
   unsigned before = 0;  // items of the sequences ahead
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     if (b0) of(b0 + lane, pages, groups);
@@ -272,16 +276,25 @@ __device__ __forceinline__ bool token_item(const WinArgs& a, const CacheArgs& c,
   return false;
 }
 
-template <int D, bool F16>
-__global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cache, float* __restrict__ parts, TokenPlan plan) {
-  constexpr int KL = D / 64, VT = D / 16;  // 16-byte loads a row of K, tiles of 16 dv
-  __shared__ float lds_o[4][16 * D];
-  __shared__ float lds_ml[4][16][2];
-  TokenItem at;
-  if (!token_item(a, cache, plan, blockIdx.x, at)) return;
+// ONE: a workgroup takes all pages of its rows.
+template <int D, bool F16, bool ONE>
+__global__ __launch_bounds__(ONE ? 512 : 256, ONE ? 1 : 2) void k_cache_token(WinArgs a, CacheArgs cache, float* __restrict__ parts, TokenPlan plan) {
+  constexpr int KL = D / 64, VT = D / 16, NW = ONE ? 8 : 4;  // 16-byte loads a row of K, tiles of 16 dv, wavefronts
+  __shared__ float lds_o[NW][16 * D];
+  __shared__ float lds_ml[NW][16][2];
+  TokenItem at = {};
+  if (ONE) {
+    at.rt = (int)blockIdx.x % plan.tiles;
+    at.hk = (int)blockIdx.x / plan.tiles % a.Hkv;
+    at.b = (int)blockIdx.x / plan.tiles / a.Hkv;
+    at.parts = 1, at.per = cache.max_pages;
+  } else if (!token_item(a, cache, plan, blockIdx.x, at)) {
+    return;
+  }
   const int rt = at.rt, hk = at.hk, b = at.b;
   const WinSeq sq = win_seq(a.rq, b);
   const int rows = min(16, sq.n * a.G - rt * 16);
+  if (ONE && rows <= 0) return;
   const int nk = __builtin_amdgcn_readfirstlane(max(0, min(cache.lens[b], cache.max_pages * kPage))), shift = nk - sq.n;
   WinWalk walk(a.mask, rt * 16 / a.G + shift, (rt * 16 + rows - 1) / a.G + shift, nk, kPage, kPage);
   walk.uniform();
@@ -293,7 +306,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cac
   const int row = rt * 16 + min(m, rows - 1), qi = row / a.G, hq = hk * a.G + row % a.G;
   const WinSpan span = win_span(a.mask, qi + shift, nk);
   // the wavefront's pages, 64 at a time, one a lane
-  const int np = p1 - p0 > wave ? (p1 - p0 - wave + 3) / 4 : 0;
+  const int np = p1 - p0 > wave ? (p1 - p0 - wave + NW - 1) / NW : 0;
   int id = -1, chunk = -1;
   float sks = 1.f, svs = 1.f;
   auto want = [&](int i) {
@@ -302,7 +315,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cac
     const int mine = chunk * 64 + lane;
     id = -1, sks = 1.f, svs = 1.f;
     if (mine < np) {
-      id = cache.table[(long long)b * cache.max_pages + walk.begin(p0 + wave + 4 * mine) / kPage];
+      id = cache.table[(long long)b * cache.max_pages + walk.begin(p0 + wave + NW * mine) / kPage];
       if ((unsigned)id >= (unsigned)cache.pages) id = -1;
       if (id >= 0) {
         sks = cache.ks[(long long)id * a.Hkv + hk];
@@ -345,7 +358,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cac
     for (int x = 0; x < VT; ++x) p.v[x] = *(const uint4*)(vp + (16 * x + m) * kPage + 16 * g);
   };
   auto multiply = [&](int i, Page& p, const Scales& sc) {
-    const int piece = p0 + wave + 4 * i, key0 = walk.begin(piece);
+    const int piece = p0 + wave + NW * i, key0 = walk.begin(piece);
     if (!sc.there) return;  // (the entry names no page: hidden)
     const float f = sc.f, lv = sc.lv;
     f32x4 s[4];
@@ -438,16 +451,16 @@ __global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cac
 #pragma unroll
   for (int x = 0; x < VT; ++x) *(f32x4*)&lds_o[wave][m * D + (((4 * x + g) ^ m) << 2)] = o[x];
   __syncthreads();
-  if (tid == 0 && at.part == 0 && !plan.one)  // for the join: where the parts are
+  if (!ONE && tid == 0 && at.part == 0)  // for the join: where the parts are
     ((int4*)(parts + (long long)plan.grid * (16 * (D + 2))))[(b * a.Hkv + hk) * plan.tiles + rt] = make_int4(at.first, at.parts, at.step, 0);
   // rows of the tile, 8 elements a thread
-  for (int it = tid; it < rows * (D / 8); it += 256) {
+  for (int it = tid; it < rows * (D / 8); it += 64 * NW) {
     const int r = it / (D / 8), ch = it % (D / 8);
     float M = lds_ml[0][r][0], L = 0.f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 1; w < 4; ++w) M = fmaxf(M, lds_ml[w][r][0]);
+    for (int w = 1; w < NW; ++w) M = fmaxf(M, lds_ml[w][r][0]);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const float f = fast_exp2(lds_ml[w][r][0] - M);
       L += f * lds_ml[w][r][1];
       const f32x4 y0 = *(const f32x4*)&lds_o[w][r * D + (((2 * ch) ^ r) << 2)], y1 = *(const f32x4*)&lds_o[w][r * D + (((2 * ch + 1) ^ r) << 2)];
@@ -455,7 +468,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_token(WinArgs a, CacheArgs cac
       for (int e = 0; e < 4; ++e) v[e] += f * y0[e], v[4 + e] += f * y1[e];
     }
     const int row_of = rt * 16 + r, q_of = row_of / a.G, h_of = hk * a.G + row_of % a.G;
-    if (at.parts == 1) {
+    if (ONE || at.parts == 1) {
       const bool none = M <= kNoRow;
       const float inv = none ? 0.f : 1.f / L;
       const uint4 u = {pack16<F16>(v[0] * inv, v[1] * inv), pack16<F16>(v[2] * inv, v[3] * inv), pack16<F16>(v[4] * inv, v[5] * inv),
@@ -525,8 +538,9 @@ __global__ __launch_bounds__(256) void k_cache_join(WinArgs a, CacheArgs cache, 
 namespace {
 template <int D, bool F16>
 hipError_t token(const WinArgs& a, const CacheArgs& c, float* parts, hipStream_t s) {
-  const TokenPlan plan = token_plan(a.B, a.H, a.Hkv, a.rq.most, c.max_pages);
-  k_cache_token<D, F16><<<(unsigned)plan.grid, 256, 0, s>>>(a, c, parts, plan);
+  const TokenPlan plan = token_plan(a.B, a.H, a.Hkv, D, a.rq.most, c.max_pages);
+  if (plan.one) k_cache_token<D, F16, true><<<(unsigned)plan.grid, 512, 0, s>>>(a, c, parts, plan);
+  else k_cache_token<D, F16, false><<<(unsigned)plan.grid, 256, 0, s>>>(a, c, parts, plan);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || plan.one) return e;
   k_cache_join<D, F16><<<(unsigned)plan.groups * 16u, 256, 0, s>>>(a, c, parts, plan);
