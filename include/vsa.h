@@ -213,7 +213,8 @@ int vsa_backward(const vsa_params_t* p, const void* q, const void* k, const void
  * log-sum-exp of -inf and no gradient.  Query head h reads key head h / (H / Hkv).
  *
  * Tensors are of bf16 or fp16 rows of d (64 or 128) elements; every row is contiguous and 16-byte aligned, batch, token and head
- * strides are free (in elements, multiples of 8, not negative; those of outputs at least d; token strides at most 2^24).
+ * strides are free (in elements, multiples of 8, not negative; token strides at most 2^24; outputs: at least d, and no two rows
+ * may overlap).  At most 2^28 rows, queries or keys, also of a table's pages; larger calls get VSA_ERR_UNSUPPORTED.
  * Dense: B sequences of max_q queries and max_k keys.  Packed: token rows of all sequences one behind the other, sequence b at
  * rows cu[b] .. cu[b+1] - 1 of total_q (total_k), the batch strides unused.  cu, lens and table are device memory and are not
  * validated: offsets are clamped to the tensors and to max_q, max_k, so that no access leaves the buffers.  Rows of an output

@@ -182,15 +182,16 @@ def vsa_window_backward(pb: WindowProblem, q, k, v, out, dout, lse, dq, dk, dv, 
 
 
 class WindowBuffers:
-    """Convenience holder: allocates every output, saved tensor and the workspace of a WindowProblem once."""
+    """Convenience holder: allocates every output, saved tensor and the workspace of a WindowProblem once.  packed: by default
+    where the problem gives total rows; to be said where packed tensors have none at all."""
 
-    def __init__(self, pb: WindowProblem, device="cuda", backward=True):
+    def __init__(self, pb: WindowProblem, device="cuda", backward=True, packed=None):
         self.pb = pb
         need = max(vsa_window_workspace_bytes(pb, False), vsa_window_workspace_bytes(pb, True) if backward else 0)
         if need == 0:
             raise ValueError(f"not a problem the library takes: {pb}")
         device = torch.empty(0, device=device).device
-        packed = pb.total_q > 0 or pb.total_k > 0
+        packed = pb.total_q > 0 or pb.total_k > 0 if packed is None else packed
         sq, sk = _shapes(pb, packed)
         new = lambda s: torch.empty(s, dtype=pb.dtype, device=device)
         self.out = new(sq)

@@ -174,6 +174,82 @@ def test_many_parts():
     attend_case(6, [30011, 70], [1, 1], 8, 1, 64, BF, (-1, 0, 0, 1), 512)
 
 
+@pytest.mark.parametrize("new", [[1, 0, 1], [40, 1, 60], [260, 0, 140]])
+@pytest.mark.parametrize("d", [64, 128])
+def test_short_calls_on_a_long_cache(new, d):
+    """Walks in parts, whichever kernel has them: single tokens, few queries, a chunk."""
+    attend_case(7, [4001, 64, 2900], new, 4, 2, d, BF, (-1, 0, 0, 1), 80)
+    attend_case(8, [4001, 64, 2900], new, 4, 2, d, FP, (2000, 0, 70, 1), 80)
+
+
+@pytest.mark.parametrize("columns", [4, 16, 17, 32, 33])
+def test_short_tables(columns):
+    """Caches that one workgroup walks alone, and the first that it does not."""
+    lens = [min(n, 64 * columns) for n in (1, 200, 1024, 1025, 2048, 2049)]
+    attend_case(9, lens, [1, 1, 3, 1, 0, 2], 4, 2, 128, BF, (-1, 0, 0, 1), columns)
+    attend_case(10, lens, [1, 1, 3, 1, 0, 2], 6, 2, 64, FP, (70, 0, 3, 1), columns)
+
+
+def test_more_sequences_than_lanes():
+    """130 sequences, some empty or without queries, tables of many and of few columns."""
+    lens = [i * 37 % 301 for i in range(130)]
+    new = [min(i % 3, n) for i, n in enumerate(lens)]
+    for columns in (5, 40):
+        attend_case(11, lens, new, 4, 2, 64, BF, (100, 0, 4, 1), columns)
+    attend_case(12, lens, [130 if i == 77 else x for i, x in enumerate(new)], 2, 2, 64, BF, (100, 0, 4, 1), 40)
+
+
+def test_parts_of_more_than_64_pages_a_wavefront():
+    """Long sequences that fill the chip by themselves; their pages repeat, so that the pool stays small."""
+    B, H, Hkv, d, n = 40, 8, 8, 64, 70399
+    k8, v8, ks, vs = filled(13, 50, Hkv, d)
+    table = torch.randint(0, 50, (B, 1101), generator=torch.Generator().manual_seed(14), dtype=torch.int32)
+    q = (randn(15, B, 1, H, d) * 0.5).to(BF)
+    lens = torch.full((B,), n, dtype=torch.int32)
+    got = cache_on_gpu(k8, v8, ks, vs).attend(q.cuda(), table.cuda(), lens.cuda())
+    for b in (0, 23, 39):
+        k, v, _ = ref.cached(k8, v8, ks, vs, table[b].tolist(), n)
+        ref.check(got[b], ref.attention(q[b], k, v, torch.ones(1, n, dtype=torch.bool))["out"], f"sequence {b}")
+
+
+def test_two_attentions_at_once():
+    """Two streams on one cache, each with a workspace of its own."""
+    Hkv, d, n = 2, 128, 3000
+    cache = cache_on_gpu(*filled(16, 100, Hkv, d))
+    tables = [torch.randperm(100, generator=torch.Generator().manual_seed(i))[:48][None].int().cuda() for i in range(2)]
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    qs = [(randn(17 + i, 1, m, 8, d) * 0.5).to(BF).cuda() for i, m in enumerate((1, 300))]
+    wants = [cache.attend(q, t, lens) for q, t in zip(qs, tables)]
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in qs], [[], []]
+    for _ in range(6):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                outs[i].append(cache.attend(qs[i], tables[i], lens))
+    torch.cuda.synchronize()
+    for want, got in zip(wants, outs):
+        assert all(torch.equal(want, t) for t in got)
+
+
+def test_timing_records_name_the_kernels():
+    """The per-call timing of the other entry points covers these."""
+    import ctypes as C
+    from paper_2505_13389_amd import vsa
+    cache = cache_on_gpu(*filled(18, 4, 2, 64))
+    table, lens = torch.tensor([[0, 2]], dtype=torch.int32, device="cuda"), torch.tensor([60], dtype=torch.int32, device="cuda")
+    k, q = randn(19, 1, 5, 2, 64).to(BF).cuda(), randn(20, 1, 5, 2, 64).to(BF).cuda()
+    lib = vsa.lib()
+    assert lib.vsa_profile_begin(8) == 0
+    cache.append(k, k, table, lens)
+    cache.attend(q, table, lens + 5)
+    torch.cuda.synchronize()
+    names = [lib.vsa_profile_name(i) for i in range(lib.vsa_profile_count())]
+    times = [lib.vsa_profile_ms(i) for i in range(lib.vsa_profile_count())]
+    assert lib.vsa_profile_end() == 0
+    names = [n.decode() if isinstance(n, bytes) else n for n in names]
+    assert len(names) == 2 and all("cache" in n for n in names) and all(0 < t < 1000 for t in times), (names, times)
+
+
 def test_pool_past_32_bits():
     """Pages behind 2^32 bytes of the pool, read and written."""
     Hkv, d, pages, last = 8, 128, 70000, 69990

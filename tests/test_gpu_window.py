@@ -80,6 +80,135 @@ def test_launches_with_a_wavefront_a_block(d, dtype):
     check_sequences(run_packed(x, lens, H, Hkv, d, mask, dtype), x, lens, mask, dtype)
 
 
+@pytest.mark.parametrize("d,dtype", [(64, FP), (128, BF)])
+@pytest.mark.parametrize("mask", [(-1, 0, 0, 1), (-1, -1, 0, 1), (900, 0, 70, 1), (3, 1, 1, 256)])
+def test_few_queries_of_many_keys(mask, d, dtype):
+    """A walk in several parts, joined; the longest sequence's queries see far more than the others', of which some see nothing."""
+    lens = [(40, 3100), (1, 2), (70, 0), (64, 2500), (130, 1)]
+    x = tensors(21, sum(l[0] for l in lens), sum(l[1] for l in lens), 2, 1, d, dtype)
+    check_sequences(run_packed(x, lens, 2, 1, d, mask, dtype, extra=2), x, lens, mask, dtype)
+
+
+def test_few_queries_of_many_keys_dense():
+    B, H, Hkv, d, mask = 2, 4, 2, 128, (-1, 0, 0, 1)
+    lens = [(33, 2100)] * B
+    x = tensors(22, 33 * B, 2100 * B, H, Hkv, d, BF)
+    q, k, v, do = (t.cuda().unflatten(0, (B, -1)) for t in x)
+    pb = window.WindowProblem(B, H, Hkv, d, 33, 2100, *mask)
+    buf = window.WindowBuffers(pb)
+    buf.forward(q, k, v)
+    buf.backward(q, k, v, do)
+    got = {n: getattr(buf, n).flatten(0, 1) for n in ("out", "dq", "dk", "dv")}
+    check_sequences(got | {"lse": buf.lse}, x, lens, mask, BF)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("mask", [(-1, 0, 0, 1), (20, 0, 9, 1), (1, 0, 1, 150)])
+@pytest.mark.parametrize("packed", [False, True])
+def test_key_blocks_that_many_queries_see(mask, d, packed):
+    """Walks of key blocks in parts (long ones, and those of sinks), the heads of a group behind each other."""
+    lens, H, Hkv = [(1500, 1500)], 4, 1
+    if packed:
+        lens = [(1500, 1500), (10, 900), (200, 64)]
+    x = tensors(23, sum(l[0] for l in lens), sum(l[1] for l in lens), H, Hkv, d, BF)
+    if packed:
+        check_sequences(run_packed(x, lens, H, Hkv, d, mask, BF, extra=1), x, lens, mask, BF)
+        return
+    pb = window.WindowProblem(1, H, Hkv, d, 1500, 1500, *mask)
+    buf = window.WindowBuffers(pb)
+    q, k, v, do = (t.cuda()[None] for t in x)
+    buf.forward(q, k, v)
+    buf.backward(q, k, v, do)
+    check_sequences({n: getattr(buf, n)[0] for n in ("out", "dq", "dk", "dv")} | {"lse": buf.lse}, x, lens, mask, BF)
+
+
+def test_many_short_sequences():
+    """More sequences than a wavefront has lanes, among them empty ones."""
+    lens = [(i * 7 % 67, i * 5 % 71) for i in range(150)]
+    mask, H, Hkv, d = (9, 2, 3, 1), 2, 2, 64
+    x = tensors(24, sum(l[0] for l in lens), sum(l[1] for l in lens), H, Hkv, d, BF)
+    check_sequences(run_packed(x, lens, H, Hkv, d, mask, BF, extra=1), x, lens, mask, BF)
+
+
+@pytest.mark.parametrize("nq,nk", [(0, 70), (70, 0), (0, 0)])
+@pytest.mark.parametrize("packed", [False, True])
+def test_no_queries_or_no_keys(nq, nk, packed):
+    B, H, Hkv, d = 2, 4, 2, 128
+    if packed:
+        pb = window.WindowProblem(B, H, Hkv, d, nq, nk, -1, 0, total_q=B * nq, total_k=B * nk)
+        cu = [torch.arange(B + 1, dtype=torch.int32, device="cuda") * n for n in (nq, nk)]
+        new = lambda n, h: torch.ones(B * n, h, d, dtype=BF, device="cuda")
+    else:
+        pb, cu = window.WindowProblem(B, H, Hkv, d, nq, nk, -1, 0), [None, None]
+        new = lambda n, h: torch.ones(B, n, h, d, dtype=BF, device="cuda")
+    buf = window.WindowBuffers(pb, packed=packed)
+    for n in ("out", "lse", "dq", "dk", "dv"):
+        getattr(buf, n).fill_(7.0)
+    q, k, v, do = new(nq, H), new(nk, Hkv), new(nk, Hkv), new(nq, H)
+    buf.forward(q, k, v, *cu)
+    buf.backward(q, k, v, do, *cu)
+    for n in ("out", "dq", "dk", "dv"):
+        assert not getattr(buf, n).any(), n
+    assert (buf.lse == float("-inf")).all()
+
+
+def test_two_calls_at_once():
+    """Two streams, each with its own buffers, the parts of both in flight together."""
+    H, Hkv, d, mask = 4, 1, 128, (-1, 0, 0, 1)
+    pb = window.WindowProblem(1, H, Hkv, d, 700, 1500, *mask)
+    xs = [[t.cuda()[None] for t in tensors(30 + i, 700, 1500, H, Hkv, d, BF)] for i in range(2)]
+    bufs, wants = [window.WindowBuffers(pb) for _ in xs], []
+    for x in xs:
+        bufs[0].forward(*x[:3])
+        bufs[0].backward(*x)
+        wants.append({n: getattr(bufs[0], n).clone() for n in ("out", "lse", "dq", "dk", "dv")})
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    for _ in range(5):
+        for x, buf, s in zip(xs, bufs, streams):
+            with torch.cuda.stream(s):
+                buf.forward(*x[:3])
+                buf.backward(*x)
+    torch.cuda.synchronize()
+    for buf, want in zip(bufs, wants):
+        for n, t in want.items():
+            assert torch.equal(getattr(buf, n), t), n
+
+
+def test_two_graphs_share_a_workspace():
+    """Replayed in turn on one stream: neither leaves anything in the workspace that the other needs."""
+    H, Hkv, d = 4, 1, 64
+    work, steps = None, []
+    for i, (n, mask) in enumerate([(900, (-1, 0, 0, 1)), (300, (50, 0, 3, 1))]):
+        pb = window.WindowProblem(1, H, Hkv, d, n, n, *mask)
+        x = [t.cuda()[None] for t in tensors(40 + i, n, n, H, Hkv, d, BF)]
+        if work is None:
+            work = torch.empty(window.vsa_window_workspace_bytes(pb, True), dtype=torch.uint8, device="cuda")
+        out, dq, dk, dv = (torch.zeros_like(t) for t in (x[0], x[0], x[1], x[1]))
+        lse = torch.zeros(H, n, device="cuda")
+
+        def step(pb=pb, x=x, out=out, lse=lse, grads=(dq, dk, dv)):
+            window.vsa_window_forward(pb, *x[:3], out, lse, workspace=work)
+            window.vsa_window_backward(pb, *x[:3], out, x[3], lse, *grads, work)
+        step()
+        torch.cuda.synchronize()
+        results = (out, lse, dq, dk, dv)
+        want = [t.clone() for t in results]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        steps.append((graph, results, want, x))  # (a graph does not keep its inputs)
+    for _ in range(4):
+        for graph, results, *_ in steps:
+            for t in results:
+                t.fill_(3.0)
+            graph.replay()
+        torch.cuda.synchronize()
+        for _, results, want, _ in steps:
+            for t, w in zip(results, want):
+                assert torch.equal(t, w)
+
+
 @pytest.mark.parametrize("layout", ["tokens", "heads", "fused", "sliced"])
 def test_dense_strides(layout):
     B, L, H, Hkv, d, mask = 3, 150, 4, 2, 128, (1, 0, 1, 30)
