@@ -280,7 +280,7 @@ typedef struct {
 /* New tokens k, v [.., Hkv, d] behind the lens[b] tokens a sequence has.  A page's scale is a power of two, the smallest that
  * brings its largest value to 448 or less (at least 2^-60; NaN and Inf are not counted and stored as NaN); where the new tokens
  * need a larger one than the page has, what it holds moves to it.  A page that is appended to must belong to one sequence only,
- * and not be read by another stream meanwhile.  Tokens beyond max_pages * 64 are dropped.
+ * stand in its table once, and not be read by another stream meanwhile.  Tokens beyond max_pages * 64 are dropped.
  *   cu  in  int32 [B+1] (packed) or NULL (dense: max_q new tokens each) */
 int vsa_cache_append(const vsa_cache_t* p, const void* k, const void* v, const int32_t* cu, const int32_t* lens,
                      const int32_t* table, void* k_pages, void* v_pages, float* k_scale, float* v_scale, void* hip_stream);

@@ -76,7 +76,7 @@ class _WindowAttention(torch.autograd.Function):
     def forward(ctx, q, k, v, cu_q, cu_k, pb):
         packed = cu_q is not None
         rows = q.shape[0] if packed else q.shape[0] * q.shape[1]
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)  # (rows of no sequence: written by nobody)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)  # (rows of no sequence: written by nobody)
         if packed:
             out.zero_()
         lse = torch.empty((pb.H, rows), dtype=torch.float32, device=q.device)
@@ -125,11 +125,11 @@ def _rows_of_16_bytes(x):
 def window_attention(q, k, v, *, left=-1, right=0, sinks=0, unit=1, softmax_scale=None, cu_q=None, cu_k=None, max_q=None, max_k=None):
     """softmax(scale q k^T over the visible keys) v.  Packed sequences: max_q and max_k bound their lengths (None: the rows of
     the tensor).  Returns a tensor of q's shape; packed, the rows of no sequence are zeros, and so are their gradients."""
+    packed = cu_q is not None
+    if q.dim() != (3 if packed else 4) or k.dim() != q.dim() or v.dim() != q.dim():
+        raise ValueError("q, k, v are [B, L, heads, d], or [rows, heads, d] with cu_q and cu_k")
     held = _refuse_held_leaves(q, k, v) if q.is_cuda and torch.cuda.is_current_stream_capturing() else None  # noqa: F841 (kept to the end)
     q, k, v = (_rows_of_16_bytes(x) for x in (q, k, v))
-    packed = cu_q is not None
-    if q.dim() != (3 if packed else 4) or k.dim() != q.dim():
-        raise ValueError("q, k, v are [B, L, heads, d], or [rows, heads, d] with cu_q and cu_k")
     B = cu_q.numel() - 1 if packed else q.shape[0]
     longest = lambda most, x: x.shape[-3] if most is None else min(most, x.shape[-3]) if packed else x.shape[-3]
     pb = window.WindowProblem(B, q.shape[-2], k.shape[-2], q.shape[-1], longest(max_q, q), longest(max_k, k), left, right, sinks, unit,

@@ -664,9 +664,10 @@ __global__ __launch_bounds__(256) void k_window_merge(WinArgs a, CacheArgs cache
 }
 
 // Wavefronts a block and parts of its walk, by the time they would take: generations of the workgroups that fit at once (a wavefront
-// takes a SIMD, 1024 in all; d = 64: half of one) times the units of one, kStart units' worth of start-up and stores each, and where there are parts what
-// writing and joining them takes.  (A unit takes about 0.7 us.  2048 tokens, two heads, d = 64: one wavefront a block 16.5 us, four 9.9;
-// 1560 queries on a cache of 32760 tokens, 12 heads, d = 128: a part each 189 us, in parts 139.)
+// takes a SIMD, 1024 in all; d = 64: half of one) times the units of one, kStart units' worth of start-up and stores each, and where
+// there are parts what writing and joining them takes.  (A unit is about 0.7 us.  2048 tokens, two heads, d = 64: one wavefront a
+// block 21 us, four 10; 1560 queries on a cache of 32760 tokens, 12 heads, d = 128: unsplit 188 us, in parts 140.  Of 38 shapes of 64
+// to 8192 queries on up to 32760 keys the plan is within 10 % of the best of one or four wavefronts, one, two or four parts.)
 static RowPlan row_plan(const WinArgs& a, long long max_k, int d) {
   constexpr long long kStart = 6, kJoin = 10;
   RowPlan best = {};
@@ -677,7 +678,7 @@ static RowPlan row_plan(const WinArgs& a, long long max_k, int d) {
       const long long places = (d == 64 ? 2048 : 1024) / nw, each = (units + nw * p - 1) / (nw * p);
       if (p > 1 && each < 4) break;
       const long long gens = (n * p + places - 1) / places;
-      const long long time = gens * (each + kStart + (nw > 1 ? 2 : 0)) + (p > 1 ? kJoin + n * p / 64 : 0);
+      const long long time = gens * (each + kStart + (nw > 1 ? 2 : 0)) + (p > 1 ? kJoin + n * p / 64 + p : 0);
       if (least < 0 || time < least) {
         least = time;
         best.nw = nw, best.parts = p, best.per = (int)((units + p - 1) / p);

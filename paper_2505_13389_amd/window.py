@@ -73,7 +73,7 @@ class WindowProblem:
 def _strides(t, name):
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
-    s = t.stride()
+    s = [step if n > 1 else 0 for n, step in zip(t.shape, t.stride())]  # (of a dimension with one entry it may be anything)
     return VsaStrides(s[0] if t.dim() == 4 else 0, s[-3], s[-2])
 
 
@@ -159,8 +159,8 @@ def _workspace(t, need, device):
     """The one given, or a new one."""
     if t is None:
         return torch.empty(need, dtype=torch.uint8, device=device)
-    if t.device != device:
-        raise ValueError("the workspace must be on the tensors' device")
+    if t.device != device or not t.is_contiguous():
+        raise ValueError("the workspace must be contiguous and on the tensors' device")
     return t
 
 
@@ -296,11 +296,12 @@ class PagedCache:
     def attend(self, q, table, lens, cu=None, max_q=None, *, left=-1, right=0, sinks=0, unit=1, softmax_scale=0.0, out=None, lse=None,
                workspace=None):
         """Attention of q over the first `lens` tokens of each sequence, of which the queries are the last: q [B, n, H, d], or packed
-        [rows, H, d] with offsets `cu` and at most `max_q` queries a sequence.  Returns out (a new tensor, or the one given); rows
+        [rows, H, d] with offsets `cu` and at most `max_q` queries a sequence (None: as many as there are rows; where all have
+        few, saying so is faster).  Returns out (a new tensor, or the one given); rows
         that belong to no sequence are not written."""
         packed = cu is not None
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape or out.dtype != q.dtype:
             raise ValueError(f"out must be {q.dtype} {tuple(q.shape)}, not {out.dtype} {tuple(out.shape)}")
         key = (q.shape, q.stride(), out.stride(), q.dtype, table.shape, lens.shape, packed and cu.shape, max_q, left, right, sinks, unit,

@@ -151,6 +151,22 @@ def test_the_binding_checks_shapes_types_and_devices():
     assert cache.workspace_bytes(1, 4, 1, 2) > 0 and cache.workspace_bytes(1, 3, 1, 2) == 0
 
 
+def test_the_binding_checks_workspaces_and_dimensions():
+    from paper_2505_13389_amd.autograd import window_attention
+    pb = window.WindowProblem(1, 2, 1, 64, 4, 6)
+    q, k = torch.zeros(1, 4, 2, 64, dtype=BF), torch.zeros(1, 6, 1, 64, dtype=BF)
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(1 << 20, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError, match="contiguous"):
+            window.vsa_window_forward(pb, q, k, k, q.clone(), workspace=ws)
+    for bad in ((q[0], k, k), (q, k[0], k), (q, k, k[0]), (q[0, 0], k[0, 0], k[0, 0])):
+        with pytest.raises(ValueError):
+            window_attention(*bad)
+    # strides of dimensions with one entry say nothing
+    odd = torch.zeros(6 * 64, dtype=BF).as_strided((1, 6, 1, 64), (3, 64, 1, 1))
+    s = window._strides(odd, "k")
+    assert (s.batch, s.token, s.head) == (0, 64, 0)
+
+
 def test_leaves_that_another_graph_holds_are_refused(monkeypatch):
     """What window_attention checks while it is captured."""
     from paper_2505_13389_amd import autograd
