@@ -10,7 +10,8 @@ namespace vsa {
 // finer scale would not make its values any more precise (only the smallest ones), dividing by a power of two is exact, and
 // so is moving a page that holds tokens to a larger scale, but for values that become subnormal.
 // A thread holds 4 tokens x 8 elements: K goes out as 8 bytes a token, V is transposed through LDS, 4 tokens to a dword.
-// Bound by HBM: 2 bytes in and 1 out a value.
+// Bound by HBM: 2 bytes in and 1 out a value.  75600 tokens, 40 heads, d = 128: 410 us, 5.7 TB/s of both ways; a frame of 1560
+// tokens for two sequences, 12 heads: 8.2 us in the kernel; a token for 16 sequences: 5.7, start, one trip to memory, the maximum and the stores.
 
 // the smallest power of two that brings `top` (finite, not negative) to 448 = 0.875 * 2^9 or less
 __device__ __forceinline__ float page_scale(float top) {
@@ -174,7 +175,9 @@ hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s) {
 // with the running maximum of x + log2(scale) as reference, so that P' stays within [0, 1] and 16 bits of either type hold it
 // as well as they would hold P; the sum of the row takes it out again, a page at a time.
 // The next page is on its way while one is multiplied.  Partial results (O, reference, sum) are joined in order by a second
-// launch where there is more than one part.  Bound by HBM: 2 d bytes a token and head.
+// launch where there is more than one part.  P' is rounded to 16 bits, half a step of each term; all else is fp32 up to O.
+// Bound by HBM: 2 d bytes a token and head.  16 sequences of 1000 to 131072 tokens, 16 heads on 4, d = 128: 103 us and 5 for the
+// join, 5.7 TB/s; four of up to 2011 tokens: 8.8 and 3.8, chains of trips to memory (lengths, table, scales, page).
 constexpr float kNoRow = -1e30f;
 
 // How the pages are dealt to workgroups.  The host knows bounds only, so the kernels work it out from the lengths: all pages that the

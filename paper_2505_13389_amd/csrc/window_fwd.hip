@@ -9,6 +9,16 @@
 // PAGED: K and V come from the pages of the 8-bit cache, as bytes, and are widened as operands.  Rows of the tile are keys in an
 // order that puts a lane's 16 values of S^T at consecutive keys, and a contraction step pair of K at 16 consecutive bytes:
 // every LDS read is 16 bytes.  K's scale goes into the softmax's factor, V's into its exponent and reference: see k_cache_token.
+//
+// Roundings: P goes to 16 bits before the product with V, half a step of each term, as in the fine kernels (a product of 32-bit
+// operands would take 16 times the matrix instructions); S, sums, references, O and log-sum-exps are fp32, and O is rounded once,
+// when it is stored.  Against 64 bits 2.3e-3 of the norm in bf16, 2.6e-4 in fp16 (rounding the exact result: 1.7e-3 and 2.0e-4).
+//
+// Bound by matrix instructions and the power they take, in small launches by start-up (about 10000 cycles from launch to the first
+// product, and the way of O out).  A unit is 1600 cycles (1024 of them the matrix pipe's; d = 64: half), PAGED 2060, 64 conversions
+// more.  32760 tokens, 12 heads, d = 128, a window of 7 frames of 1560: 2000 to 2050 us, 1.02 to 1.05 PFLOP/s on the visible pairs, the
+// pipe busy 58 % at 1.48 GHz; 16384 tokens, 5 frames of 1024: 460 us; packed texts of 13385 tokens, 16 heads, fp16: 131 to 135;
+// 1560 queries on the cache of 32760 tokens: 139.
 #include <type_traits>
 
 #include "ticks.h"
