@@ -212,6 +212,52 @@ def test_parts_of_more_than_64_pages_a_wavefront():
         ref.check(got[b], ref.attention(q[b], k, v, torch.ones(1, n, dtype=torch.bool))["out"], f"sequence {b}")
 
 
+def test_lengths_that_lie_stay_in_bounds():
+    """Lengths below zero or beyond the table are taken as its ends; pages of no table stay as they were."""
+    Hkv, d, columns = 2, 64, 3
+    pool = filled(21, 12, Hkv, d)
+    table = torch.tensor([[1, 3, 5], [7, 9, 11], [0, 2, 4]], dtype=torch.int32, device="cuda")
+    wrong = torch.tensor([-9, 2 ** 31 - 1, 40], dtype=torch.int32, device="cuda")
+    right = torch.tensor([0, 64 * columns, 40], dtype=torch.int32, device="cuda")
+    for n in (1, 150):
+        k, v, q = (randn(22 + i, 3, n, h, d).to(BF).cuda() for i, h in enumerate((Hkv, Hkv, 4)))
+        a, b = cache_on_gpu(*pool), cache_on_gpu(*pool)
+        a.append(k, v, table, wrong)
+        b.append(k, v, table, right)
+        for x, y in ((a.k.view(torch.uint8), b.k.view(torch.uint8)), (a.v.view(torch.uint8), b.v.view(torch.uint8)), (a.k_scale, b.k_scale)):
+            assert torch.equal(x, y)
+        for t in (a.k, a.v):
+            untouched = [6, 7, 8, 9, 10, 11]  # of no table, or behind the second sequence's last page
+            assert torch.equal(t[untouched].view(torch.uint8).cpu(), (pool[0] if t is a.k else pool[1])[untouched].view(torch.uint8))
+        assert torch.equal(a.attend(q, table, wrong), b.attend(q, table, right))
+
+
+def test_two_graphs_share_a_workspace():
+    """Single tokens and a chunk, captured over one workspace and replayed in turn."""
+    Hkv, d = 2, 128
+    cache = cache_on_gpu(*filled(25, 60, Hkv, d))
+    table = torch.randperm(60, generator=torch.Generator().manual_seed(26))[:40][None].int().cuda()
+    lens = torch.tensor([2500], dtype=torch.int32, device="cuda")
+    work = torch.empty(max(cache.workspace_bytes(1, 8, n, 40) for n in (1, 200)), dtype=torch.uint8, device="cuda")
+    steps = []
+    for n in (1, 200):
+        q = (randn(27 + n, 1, n, 8, d) * 0.5).to(BF).cuda()
+        want, out = cache.attend(q, table, lens, workspace=work).clone(), torch.zeros_like(q)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            cache.attend(q, table, lens, out=out, workspace=work)
+        steps.append((graph, out, want, q))
+    for _ in range(4):
+        work.fill_(0xFF)
+        for graph, out, *_ in steps:
+            out.fill_(3.0)
+            graph.replay()
+        torch.cuda.synchronize()
+        for _, out, want, _ in steps:
+            assert torch.equal(out, want)
+
+
 def test_two_attentions_at_once():
     """Two streams on one cache, each with a workspace of its own."""
     Hkv, d, n = 2, 128, 3000
