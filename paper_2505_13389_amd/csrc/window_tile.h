@@ -108,9 +108,9 @@ struct RowCopy {
   __device__ __forceinline__ void piece(const unsigned char* base, int c) const {
     const unsigned char* g = c < 4 ? base : base + 4 * TL::RPI * (long long)stride;
     if (c % 4 == 0) lds_dma16_at<0>(g, off[c % 4]);
-    if (c % 4 == 1) lds_dma16_at<1024>(g, off[c % 4]);
-    if (c % 4 == 2) lds_dma16_at<2048>(g, off[c % 4]);
-    if (c % 4 == 3) lds_dma16_at<3072>(g, off[c % 4]);
+    if (c % 4 == 1) lds_dma16_at<1 * 1024>(g, off[c % 4]);
+    if (c % 4 == 2) lds_dma16_at<2 * 1024>(g, off[c % 4]);
+    if (c % 4 == 3) lds_dma16_at<3 * 1024>(g, off[c % 4]);
   }
   // all of it; `have` rows are there: the last of them stands for those behind it
   __device__ __forceinline__ void all(const unsigned char* base, unsigned lds, int lane, int have) const {
