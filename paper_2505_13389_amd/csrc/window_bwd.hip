@@ -14,7 +14,7 @@
 // Bound by matrix instructions and power at d = 128 (a unit 2340 cycles in dQ, 3050 in dK/dV, of which the matrix pipe 1536 and 2048);
 // at d = 64, where P and dS take half of a unit's issue slots, by instruction issue and by start and end of walks.  16384 tokens, 12 heads,
 // d = 128, 5 frames of 1024: rows' terms 23 us, both passes 1403, 0.80 PFLOP/s on the visible pairs, the pipe busy 58 % at 1.7 GHz; packed
-// texts of 10332 tokens, 16 heads on 4, d = 64, 511 tokens back: 11, 147 and 5 for the join.
+// texts of 10332 tokens, 16 heads on 4, d = 64, 511 tokens back: 11, 136 and 5 for the join.
 #include <type_traits>
 
 #include "unit_stream.h"
@@ -45,17 +45,16 @@ __global__ __launch_bounds__(256) void k_window_stats(WinArgs a) {
   a.stats[n + h * a.lse_rows + row] = -sum;
 }
 
-// Accumulators in the accumulation registers (256 + 256 registers a wavefront at d = 128, see mfma_a).
+// dQ, dK, dV lie in the accumulation registers (256 + 256 registers a wavefront, see mfma_a): at d = 64, left to the compiler, parts of
+// them were moved there and back in every unit (packed training 188 us, 183 so).
 template <int D, bool F16>
 __device__ __forceinline__ void mm_acc(f32x16& acc, bf16x8 a, bf16x8 b) {
-  if constexpr (D == 64) acc = mm32<F16>(a, b, acc);
-  else if constexpr (F16) asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+  if constexpr (F16) asm volatile("v_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
   else mfma_a(acc, a, b);
 }
 template <int D>
 __device__ __forceinline__ void pin_acc(f32x16& acc) {
-  if (D == 128) asm volatile("" : "+a"(acc));
-  else asm volatile("" : "+v"(acc));
+  asm volatile("" : "+a"(acc));
 }
 // accumulators in ordinary registers, from the values of c (INIT), or on
 template <int D, bool F16, bool INIT>
@@ -152,7 +151,7 @@ __device__ __forceinline__ void store_part(f32x16 (&acc)[D / 32][2], float* buf,
 // K has three stages (of unit u to its end, of u + 1, of u + 2), V two.
 template <int D, int NW>
 struct DqShape {
-  static constexpr int PLACE = (D == 64 ? 4 : 5) * 32 * D * 2;  // of a wavefront
+  static constexpr int PLACE = 5 * 32 * D * 2;  // of a wavefront
   static constexpr int LDS = NW * PLACE;
 };
 template <int D, bool F16, int NW>
@@ -187,7 +186,7 @@ __device__ __forceinline__ void dq_block(unsigned char* smem, const WinArgs& a, 
   auto copy_all = [&](const RowCopy<D>& c, const unsigned char* base, int key, unsigned lds) {
     c.all(base + (long long)key * c.stride, lds, lane, nk - key);
   };
-  constexpr int kV = (D == 64 ? 2 : 3) * HALF;  // of the V stages
+  constexpr int kV = 3 * HALF;  // of the V stages
 
   // the first copies, then Q and dO, then what can be done while they are on their way
   if (nu > 0) {
@@ -307,50 +306,6 @@ __device__ __forceinline__ void dq_block(unsigned char* smem, const WinArgs& a, 
     }
   asm volatile("" : "+v"(from[0]), "+v"(from[1]), "+v"(minus[0]), "+v"(minus[1]));
 
-  if constexpr (D == 64) {
-    // Two wavefronts on a SIMD, each the vector work behind the other's products: in plain order, in half the registers.
-    for (int u = 0; u < nu; ++u) {
-      const unsigned char *ks = mine + (u & 1) * HALF, *vs = mine + kV + (u & 1) * HALF;
-      win_wait<2 * NC>();
-      f32x16 S[2], dp[2];
-#pragma unroll
-      for (int st = 0; st < KS; ++st) {
-        const bf16x8 ka = TL::rowmajor_at(ks, lane_a, st), va = TL::rowmajor_at(vs, lane_a, st);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (st == 0) mm_v_zero<D, F16>(S[t], ka, qreg[t][st]), mm_v_zero<D, F16>(dp[t], va, dreg[t][st]);
-          else mm_v<D, F16, false>(S[t], ka, qreg[t][st], S[t]), mm_v<D, F16, false>(dp[t], va, dreg[t][st], dp[t]);
-        }
-      }
-      if (__builtin_expect(walk.masked(wave + NW * u), 0)) hide(S, u);
-#pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        bf16x8 ds[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          uint32_t w[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int e = 8 * st + 2 * i;
-            const float p0 = fast_exp2(fmaf(S[t][e], sl2, from[t])), p1 = fast_exp2(fmaf(S[t][e + 1], sl2, from[t]));
-            w[i] = pack16<F16>(p0 * (dp[t][e] + minus[t]), p1 * (dp[t][e + 1] + minus[t]));
-          }
-          ds[t] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-        }
-#pragma unroll
-        for (int x = 0; x < DVB; ++x) {
-          const bf16x8 ka = TL::transposed_at(ks, b0, b1, st, x);
-#pragma unroll
-          for (int t = 0; t < 2; ++t) mm_acc<D, F16>(acc[x][t], ka, ds[t]);
-        }
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the stages have been read and may be filled again)
-      __builtin_amdgcn_sched_barrier(0);
-      copy_all(kc, kb, first_key(u + 2), lds0 + (u & 1) * HALF);
-      copy_all(vc, vb, first_key(u + 2), lds0 + kV + (u & 1) * HALF);
-    }
-    win_wait<0>();
-  } else {
   f32x16 s0[2], s1[2];
   unsigned k_at = 0;  // stage of K(u), bytes
   auto after = [](unsigned x) { return x == 2u * HALF ? 0u : x + HALF; };
@@ -427,7 +382,7 @@ __device__ __forceinline__ void dq_block(unsigned char* smem, const WinArgs& a, 
       __builtin_amdgcn_sched_barrier(0);
     });
     if (more && __builtin_expect(walk.masked(wave + NW * min(u + 1, nu - 1)), 0)) {
-      if (D == 128) mfma_fence();
+      mfma_fence();
       hide(T, u + 1);
     }
     if (!STEADY) copy_all(vc, vb, key2, lds0 + kV + par * HALF);
@@ -462,7 +417,7 @@ __device__ __forceinline__ void dq_block(unsigned char* smem, const WinArgs& a, 
       p_slots(T, n0, n1);
       __builtin_amdgcn_sched_barrier(0);
     });
-    if (D == 128 && !STEADY) mfma_fence();  // (accumulators may be moved between one form of this and another)
+    if (!STEADY) mfma_fence();  // (accumulators may be moved between one form of this and another)
     k_at = k1;
   };
   if (nu > 0) {
@@ -474,14 +429,13 @@ __device__ __forceinline__ void dq_block(unsigned char* smem, const WinArgs& a, 
       body(std::true_type{}, 0, s0, s1, u);
       body(std::true_type{}, 1, s1, s0, u + 1);
     }
-    if (D == 128) mfma_fence();
+    mfma_fence();
     for (; u < nu; ++u) {  // (behind the last unit: that one again)
       body(std::false_type{}, u & 1, s0, s1, u);
       s0[0] = s1[0];
       s0[1] = s1[1];
     }
     win_wait<0>();
-  }
   }
   mfma_fence();
 #pragma unroll
@@ -888,7 +842,7 @@ __device__ __forceinline__ void dkv_block(unsigned char* smem, const WinArgs& a,
       if (j < half) d_slots(14 + 3 * j / half, 14 + 3 * (j + 1) / half);
       __builtin_amdgcn_sched_barrier(0);
     });
-    if (D == 128 && !STEADY) mfma_fence();
+    if (!STEADY) mfma_fence();
     cur = n1;
     n1 = n2;
   };
@@ -900,7 +854,7 @@ __device__ __forceinline__ void dkv_block(unsigned char* smem, const WinArgs& a,
       body(std::true_type{}, 0, u);
       body(std::true_type{}, 1, u + 1);
     }
-    if (D == 128) mfma_fence();
+    mfma_fence();
     for (; u < nu; ++u) body(std::false_type{}, u & 1, u);
     win_wait<0>();
   }
@@ -924,7 +878,7 @@ __device__ __forceinline__ void dkv_block(unsigned char* smem, const WinArgs& a,
 }
 
 // Both passes in one launch, dK/dV's workgroups first: dQ's fill what they leave of the chip (packed training of 10332 tokens, d = 64:
-// 216 us with a launch each, 201 so; 16 frames of 1024 tokens, 12 heads, d = 128: 1901 and 1805).  NW = 4: the four wavefronts share a
+// 216 us with a launch each, 201 so, both before their walks at d = 64 became as they are; 16 frames of 1024 tokens, 12 heads, d = 128: 1901 and 1805).  NW = 4: the four wavefronts share a
 // block of queries too; NW = 2: each takes one of its own.
 template <int D, bool F16, int NW>
 __global__ __launch_bounds__(64 * NW, 1) void k_window_dq_dkv(WinArgs a, RowPlan rows, DkvPlan plan, float* __restrict__ parts, unsigned first) {
